@@ -283,9 +283,9 @@ def _run_rotate(st):
 
 
 def _codes(x):
-    """bf16 rows -> (codes, scales), both divisions and the rounding in 32 bits."""
+    """bf16 rows -> (codes, scales): each a quotient rounded to 32 bits once, then the code to a whole number."""
     x = x.float()
-    scale = x.abs().amax(-1) / 127
+    scale = (x.abs().amax(-1).double() / 127).float()      # (in 32 bits torch multiplies by 1 / 127, which is rounded twice)
     return (x / torch.where(scale > 0, scale, 1.0)[..., None]).round().clamp(-127, 127).to(torch.int8), scale
 
 

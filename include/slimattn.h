@@ -51,7 +51,8 @@ enum {
     SLIM_ERR_UNSUPPORTED = 3, /* head_dim not in {64, 128}, or an unknown dtype code */
     SLIM_ERR_ALIGN = 4,       /* a pointer is not 16-byte aligned */
     SLIM_ERR_WORKSPACE = 5,   /* workspace smaller than the entry point's *_workspace_bytes() */
-    SLIM_ERR_LAUNCH = 6       /* the HIP runtime refused a kernel launch */
+    SLIM_ERR_LAUNCH = 6,      /* the HIP runtime refused a kernel launch */
+    SLIM_ERR_OVERLAP = 7      /* a result overlaps another buffer of a call that says it must not */
 };
 
 enum { SLIM_BF16 = 0, SLIM_F32 = 1, SLIM_I8 = 2 };
@@ -252,6 +253,46 @@ int slim_attn_decode_int8_varlen(const void* q_bf16, const int8_t* k_codes, cons
                                  void* out_bf16, void* workspace, size_t workspace_bytes,
                                  int batch, int q_heads, int kv_heads, int kv_len, int head_dim,
                                  int causal, float softmax_scale, void* stream);
+
+/*
+ * Norm and rotation of the queries and keys of batch x seq_len tokens, from the rows that a projection gives to the layout of
+ * the attention calls.  For every token (b, s) and every query head, with x its row of head_dim values:
+ *     y_d = x_d * q_weight_d / sqrt(mean_d(x_d^2) + eps)                    (q_weight NULL: y = x)
+ *     (y_i, y_j) -> (y_i c - y_j s, y_j c + y_i s),   c = cos_sin[p][i'], s = cos_sin[p][head_dim/2 + i'],  p = positions[b,s]
+ * where pair i' of head_dim/2 is (i, j) = (i', i' + head_dim/2), or (2 i', 2 i' + 1) with interleaved == 1.  Keys likewise with
+ * k_weight; values are only moved.  Every result is the exact value, as 64-bit arithmetic gives it, rounded to fp32 and then
+ * to bf16.  A token whose position lies outside [0, table_len) (the padding of a batch: -1) gets rows of zeros.
+ * q, k, v   device, in   rows of q_heads (k, v: kv_heads) x head_dim bf16, densely packed for each token; token b * seq_len + s
+ *           begins q_stride (k_stride, v_stride) values after the one before: a multiple of 8, at least the row's own length
+ *           and below 2^31.  (One projection's output [batch, seq_len, q_heads + 2 kv_heads, head_dim] is three such tensors.)
+ * q_weight, k_weight  device, in  [head_dim] bf16, or NULL
+ * cos_sin   device, in   [table_len, head_dim] fp32
+ * positions device, in   [batch, seq_len] int32, 4-byte aligned
+ * q_out, k_out, v_out  device, out  [batch, q_heads (kv_heads), seq_len, head_dim] bf16; none may overlap another buffer
+ * eps       finite and > 0 (SLIM_ERR_SHAPE otherwise), interleaved 0 or 1
+ */
+int slim_qk_norm_rope(const void* q_bf16, const void* k_bf16, const void* v_bf16, int64_t q_stride, int64_t k_stride,
+                      int64_t v_stride, const void* q_weight_bf16, const void* k_weight_bf16, const float* cos_sin,
+                      const int32_t* positions, void* q_out_bf16, void* k_out_bf16, void* v_out_bf16,
+                      int batch, int q_heads, int kv_heads, int seq_len, int head_dim, int table_len, int interleaved,
+                      double eps, void* stream);
+
+/*
+ * The same for tokens whose K and V go into an INT8 cache: queries as in slim_qk_norm_rope; token (b, s)'s codes and scales,
+ * those of kv_quant_int8 on the rows that slim_qk_norm_rope gives, bit for bit, are written at token index slots[b] + s of
+ * that sequence's cache.  (A slot is not a position: a cache that tokens were evicted from is shorter than its sequence.)
+ * A token without a position (outside [0, table_len)) or without room (slots[b] + s outside [0, kv_len)) leaves the cache as
+ * it was; the former's query is a row of zeros.  seq_len == 1 is the step before a decode.
+ * slots     device, in      [batch] int32, 4-byte aligned
+ * k_codes, v_codes  device, in/out  [batch, kv_heads, kv_len, head_dim] int8;  k_scale, v_scale  [batch, kv_heads, kv_len] fp32
+ * q_out and the caches must not overlap another buffer.  Everything else as in slim_qk_norm_rope.
+ */
+int slim_qk_norm_rope_append_int8(const void* q_bf16, const void* k_bf16, const void* v_bf16, int64_t q_stride, int64_t k_stride,
+                                  int64_t v_stride, const void* q_weight_bf16, const void* k_weight_bf16, const float* cos_sin,
+                                  const int32_t* positions, const int32_t* slots, void* q_out_bf16,
+                                  int8_t* k_codes, float* k_scale, int8_t* v_codes, float* v_scale,
+                                  int batch, int q_heads, int kv_heads, int seq_len, int kv_len, int head_dim, int table_len,
+                                  int interleaved, double eps, void* stream);
 
 /* Name of a status code; pointer to static storage, never NULL. */
 const char* slim_status_string(int status);

@@ -43,6 +43,20 @@ int check_shape(int batch, int q_heads, int kv_heads, int len, int head_dim) {
     return SLIM_OK;
 }
 
+// Whether any of the n_out first ranges overlaps another one of the n
+struct Range {
+    const void* p;
+    size_t bytes;
+};
+bool any_overlap(const Range* r, int n_out, int n) {
+    for (int i = 0; i < n_out; ++i)
+        for (int j = 0; j < n; ++j) {
+            const uintptr_t a = (uintptr_t)r[i].p, b = (uintptr_t)r[j].p;
+            if (i != j && a < b + r[j].bytes && b < a + r[i].bytes) return true;
+        }
+    return false;
+}
+
 }  // namespace
 
 extern "C" {
@@ -56,6 +70,7 @@ const char* slim_status_string(int status) {
         case SLIM_ERR_ALIGN: return "SLIM_ERR_ALIGN: pointers must be 16-byte aligned";
         case SLIM_ERR_WORKSPACE: return "SLIM_ERR_WORKSPACE: workspace too small";
         case SLIM_ERR_LAUNCH: return "SLIM_ERR_LAUNCH: kernel launch failed";
+        case SLIM_ERR_OVERLAP: return "SLIM_ERR_OVERLAP: a result overlaps another buffer of the call";
         default: return "unknown status";
     }
 }
@@ -314,6 +329,88 @@ int slim_attn_decode_int8_varlen(const void* q_bf16, const int8_t* k_codes, cons
     if (!kv_lens) return SLIM_ERR_NULL;
     return decode_common(q_bf16, k_codes, k_scale, v_codes, v_scale, kv_lens, out_bf16, workspace, workspace_bytes, batch,
                          q_heads, kv_heads, kv_len, head_dim, causal, softmax_scale, stream);
+}
+
+// What the two calls share
+static int rope_common(slim::RopeArgs& a, bool append, hipStream_t stream) {
+    if (!a.q || !a.k || !a.v || !a.cos_sin || !a.positions || !a.q_out) return SLIM_ERR_NULL;
+    if (append ? (!a.slots || !a.k_codes || !a.k_scale || !a.v_codes || !a.v_scale) : (!a.k_out || !a.v_out)) return SLIM_ERR_NULL;
+    int st = check_shape(a.batch, a.q_heads, a.kv_heads, a.seq_len, a.head_dim);
+    if (st == SLIM_OK) st = check_shape(a.batch, a.kv_heads, a.kv_heads, a.kv_len, a.head_dim);
+    if (st != SLIM_OK) return st;
+    if (a.table_len <= 0 || !(a.eps > 0.0) || !isfinite(a.eps)) return SLIM_ERR_SHAPE;
+    const long q_row = (long)a.q_heads * a.head_dim, kv_row = (long)a.kv_heads * a.head_dim, lim = 2147483647L;
+    if (a.q_stride < q_row || a.k_stride < kv_row || a.v_stride < kv_row) return SLIM_ERR_SHAPE;
+    if (a.q_stride > lim || a.k_stride > lim || a.v_stride > lim) return SLIM_ERR_SHAPE;
+    if ((a.q_stride | a.k_stride | a.v_stride) & 7) return SLIM_ERR_ALIGN;
+    if (misaligned(a.q) || misaligned(a.k) || misaligned(a.v) || misaligned(a.q_weight) || misaligned(a.k_weight) ||
+        misaligned(a.cos_sin) || misaligned(a.q_out))
+        return SLIM_ERR_ALIGN;
+    if (append ? (misaligned(a.k_codes) || misaligned(a.k_scale) || misaligned(a.v_codes) || misaligned(a.v_scale))
+               : (misaligned(a.k_out) || misaligned(a.v_out)))
+        return SLIM_ERR_ALIGN;
+    if (((uintptr_t)a.positions & 3u) || ((uintptr_t)a.slots & 3u)) return SLIM_ERR_ALIGN;
+    const size_t tokens = (size_t)a.batch * a.seq_len, rows = (size_t)a.batch * a.kv_heads * a.kv_len;
+    const size_t weight = (size_t)a.head_dim * 2;
+    auto span = [&](long stride, long row) { return ((tokens - 1) * stride + row) * 2; };
+    Range r[13];
+    int n = 0;
+    r[n++] = Range{a.q_out, tokens * q_row * 2};
+    if (append) {
+        r[n++] = Range{a.k_codes, rows * a.head_dim};
+        r[n++] = Range{a.v_codes, rows * a.head_dim};
+        r[n++] = Range{a.k_scale, rows * 4};
+        r[n++] = Range{a.v_scale, rows * 4};
+    } else {
+        r[n++] = Range{a.k_out, tokens * kv_row * 2};
+        r[n++] = Range{a.v_out, tokens * kv_row * 2};
+    }
+    const int n_out = n;
+    r[n++] = Range{a.q, span(a.q_stride, q_row)};
+    r[n++] = Range{a.k, span(a.k_stride, kv_row)};
+    r[n++] = Range{a.v, span(a.v_stride, kv_row)};
+    r[n++] = Range{a.cos_sin, (size_t)a.table_len * a.head_dim * 4};
+    r[n++] = Range{a.positions, tokens * 4};
+    if (append) r[n++] = Range{a.slots, (size_t)a.batch * 4};
+    if (a.q_weight) r[n++] = Range{a.q_weight, weight};
+    if (a.k_weight) r[n++] = Range{a.k_weight, weight};
+    if (any_overlap(r, n_out, n)) return SLIM_ERR_OVERLAP;
+    drop_stale_hip_error();
+    return slim::launch_qk_norm_rope(a, append, stream) == hipSuccess ? SLIM_OK : SLIM_ERR_LAUNCH;
+}
+
+int slim_qk_norm_rope(const void* q_bf16, const void* k_bf16, const void* v_bf16, int64_t q_stride, int64_t k_stride,
+                      int64_t v_stride, const void* q_weight_bf16, const void* k_weight_bf16, const float* cos_sin,
+                      const int32_t* positions, void* q_out_bf16, void* k_out_bf16, void* v_out_bf16, int batch, int q_heads,
+                      int kv_heads, int seq_len, int head_dim, int table_len, int interleaved, double eps, void* stream) {
+    if (interleaved != 0 && interleaved != 1) return SLIM_ERR_SHAPE;
+    slim::RopeArgs a = {};
+    a.q = q_bf16, a.k = k_bf16, a.v = v_bf16;
+    a.q_stride = q_stride, a.k_stride = k_stride, a.v_stride = v_stride;
+    a.q_weight = q_weight_bf16, a.k_weight = k_weight_bf16;
+    a.cos_sin = cos_sin, a.positions = positions;
+    a.q_out = q_out_bf16, a.k_out = k_out_bf16, a.v_out = v_out_bf16;
+    a.batch = batch, a.q_heads = q_heads, a.kv_heads = kv_heads, a.seq_len = seq_len, a.head_dim = head_dim;
+    a.kv_len = seq_len, a.table_len = table_len, a.interleaved = interleaved == 1, a.eps = eps;
+    return rope_common(a, false, (hipStream_t)stream);
+}
+
+int slim_qk_norm_rope_append_int8(const void* q_bf16, const void* k_bf16, const void* v_bf16, int64_t q_stride, int64_t k_stride,
+                                  int64_t v_stride, const void* q_weight_bf16, const void* k_weight_bf16, const float* cos_sin,
+                                  const int32_t* positions, const int32_t* slots, void* q_out_bf16, int8_t* k_codes,
+                                  float* k_scale, int8_t* v_codes, float* v_scale, int batch, int q_heads, int kv_heads,
+                                  int seq_len, int kv_len, int head_dim, int table_len, int interleaved, double eps, void* stream) {
+    if (interleaved != 0 && interleaved != 1) return SLIM_ERR_SHAPE;
+    slim::RopeArgs a = {};
+    a.q = q_bf16, a.k = k_bf16, a.v = v_bf16;
+    a.q_stride = q_stride, a.k_stride = k_stride, a.v_stride = v_stride;
+    a.q_weight = q_weight_bf16, a.k_weight = k_weight_bf16;
+    a.cos_sin = cos_sin, a.positions = positions, a.slots = slots;
+    a.q_out = q_out_bf16;
+    a.k_codes = k_codes, a.k_scale = k_scale, a.v_codes = v_codes, a.v_scale = v_scale;
+    a.batch = batch, a.q_heads = q_heads, a.kv_heads = kv_heads, a.seq_len = seq_len, a.head_dim = head_dim;
+    a.kv_len = kv_len, a.table_len = table_len, a.interleaved = interleaved == 1, a.eps = eps;
+    return rope_common(a, true, (hipStream_t)stream);
 }
 
 }  // extern "C"

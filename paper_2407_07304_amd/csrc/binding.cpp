@@ -10,6 +10,7 @@
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>
 #include <c10/core/DefaultDtype.h>
+#include <c10/core/DeviceGuard.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -370,6 +371,106 @@ PyObject* decode_static(Args a) {
     return give(a[6], out);
 }
 
+// The calls below take tensors of any one device: that device's current stream, and results on it.
+void require_one_device(std::initializer_list<PyObject*> all) {
+    const at::Tensor* first = nullptr;
+    for (PyObject* o : all) {
+        if (!given(o)) continue;
+        const at::Tensor& t = tensor(o);
+        if (first == nullptr) first = &t;
+        require(t.device() == first->device(), "tensors on one device");
+    }
+}
+
+// Rows [B, S, heads, D] bf16 whose tokens are at one stride (in values): a token's rows densely packed
+struct TokenRows {
+    int64_t b, s, h, d, stride;
+    void* p = nullptr;
+    explicit TokenRows(const at::Tensor& t) {
+        const Dims4 n = dims4(t);
+        b = n.b, s = n.h, h = n.s, d = n.d;
+        const auto st = t.strides();
+        stride = s > 1 ? st[1] : b > 1 ? st[0] : h * d;
+        require((d <= 1 || st[3] == 1) && (h <= 1 || st[2] == d) && (s <= 1 || b <= 1 || st[0] == s * st[1]),
+                "rows of a token densely packed, tokens at one stride");
+    }
+    void take_pointer(const at::Tensor& t) {
+        require(t.is_cuda(), "device tensors, densely packed");
+        require(t.scalar_type() == at::kBFloat16, "expected torch.bfloat16");
+        p = t.data_ptr();
+    }
+};
+double as_double(PyObject* o) {
+    const double v = PyFloat_AsDouble(o);
+    if (v == -1.0 && PyErr_Occurred()) throw Failed();
+    return v;
+}
+
+// q, k, v, cos_sin, positions, and then (APPEND) slots, k_codes, k_scale, v_codes, v_scale, and then q_weight, k_weight, eps,
+// interleaved, q_out, and then (not APPEND) k_out, v_out
+template <bool APPEND>
+PyObject* qk_norm_rope(Args a) {
+    const at::Tensor &qt = tensor(a[0]), &kt = tensor(a[1]), &vt = tensor(a[2]), &table = tensor(a[3]), &positions = tensor(a[4]);
+    Args tail = a + (APPEND ? 10 : 5);
+    TokenRows q(qt), k(kt), v(vt);
+    require(k.b == q.b && k.s == q.s && k.d == q.d, "q and k of the same tokens");
+    require(vt.sizes() == kt.sizes(), "k and v have one shape");
+    require(table.dim() == 2 && table.size(1) == q.d, "cos_sin is [length, D]");
+    require_shape(positions, {q.b, q.s}, "one position per token");
+    for (int i = 0; i < 2; ++i)
+        if (given(tail[i])) require_shape(tensor(tail[i]), {q.d}, "one weight per value of a head");
+    require_one_device({a[0], a[1], a[2], a[3], a[4], tail[0], tail[1], tail[4]});
+    int64_t kv_len = q.s;
+    if (APPEND) {
+        const Dims4 c = dims4(tensor(a[6]));
+        kv_len = c.s;
+        require_shape(tensor(a[5]), {q.b}, "one slot per sequence");
+        require_shape(tensor(a[6]), {q.b, k.h, kv_len, q.d}, "shape of k_codes");
+        require(tensor(a[8]).sizes() == tensor(a[6]).sizes(), "k_codes and v_codes have one shape");
+        require_shape(tensor(a[7]), {q.b, k.h, kv_len}, "shape of k_scale");
+        require_shape(tensor(a[9]), {q.b, k.h, kv_len}, "shape of v_scale");
+        require_one_device({a[0], a[5], a[6], a[7], a[8], a[9]});
+    } else {
+        require_one_device({a[0], tail[5], tail[6]});
+    }
+    q.take_pointer(qt), k.take_pointer(kt), v.take_pointer(vt);
+    const c10::DeviceGuard guard(qt.device());
+    at::Tensor out[3];
+    out[0] = out_or_new(tail[4], {q.b, q.h, q.s, q.d}, at::kBFloat16, qt);
+    require_shape(out[0], {q.b, q.h, q.s, q.d}, "shape of q_out");
+    if (!APPEND)
+        for (int i = 1; i < 3; ++i) {
+            out[i] = out_or_new(tail[4 + i], {q.b, k.h, q.s, q.d}, at::kBFloat16, qt);
+            require_shape(out[i], {q.b, k.h, q.s, q.d}, i == 1 ? "shape of k_out" : "shape of v_out");
+        }
+    const float* const tp = f32_ptr(table);
+    const int32_t* const pp = i32_ptr(positions);
+    void* const qw = given(tail[0]) ? bf16_ptr(tensor(tail[0])) : nullptr;
+    void* const kw = given(tail[1]) ? bf16_ptr(tensor(tail[1])) : nullptr;
+    const double eps = as_double(tail[2]);
+    const int pairs = as_flag(tail[3]), B = c_int(q.b), Hq = c_int(q.h), Hkv = c_int(k.h), S = c_int(q.s), D = c_int(q.d);
+    const int L = c_int(table.size(0));
+    void* const qo = bf16_ptr(out[0]);
+    if constexpr (APPEND) {
+        const int32_t* const sp = i32_ptr(tensor(a[5]));
+        int8_t *const kc = i8_ptr(tensor(a[6])), *const vc = i8_ptr(tensor(a[8]));
+        float *const ks = f32_ptr(tensor(a[7])), *const vs = f32_ptr(tensor(a[9]));
+        call([&](void* stream) {
+            return slim_qk_norm_rope_append_int8(q.p, k.p, v.p, q.stride, k.stride, v.stride, qw, kw, tp, pp, sp, qo, kc, ks, vc, vs, B, Hq,
+                                                 Hkv, S, c_int(kv_len), D, L, pairs, eps, stream);
+        });
+        return give(tail[4], out[0]);
+    } else {
+        void *const ko = bf16_ptr(out[1]), *const vo = bf16_ptr(out[2]);
+        call([&](void* stream) {
+            return slim_qk_norm_rope(q.p, k.p, v.p, q.stride, k.stride, v.stride, qw, kw, tp, pp, qo, ko, vo, B, Hq, Hkv, S, D, L, pairs, eps,
+                                     stream);
+        });
+        PyObject* items[3] = {give(tail[4], out[0]), give(tail[5], out[1]), give(tail[6], out[2])};
+        return tuple_of(items);
+    }
+}
+
 template <PyObject* (*F)(Args), int N>
 PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
     if (n != N) {
@@ -403,6 +504,8 @@ PyMethodDef g_methods[] = {
     SLIM_ENTRY("decode", decode<false>, 9),
     SLIM_ENTRY("decode_varlen", decode<true>, 10),
     SLIM_ENTRY("decode_static", decode_static, 8),
+    SLIM_ENTRY("qk_norm_rope", qk_norm_rope<false>, 12),
+    SLIM_ENTRY("qk_norm_rope_append", qk_norm_rope<true>, 15),
     {"set_raise_status", set_raise_status, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_slimbind", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};

@@ -14,6 +14,25 @@ hipError_t launch_kv_quant_int8_pair(const void* k, const void* v, int8_t* k_cod
 hipError_t launch_kv_quant_int8_append(const void* x, int8_t* codes, float* scales, const int* positions, int batch,
                                        int kv_heads, int kv_len, int head_dim, hipStream_t stream);
 
+// Norm and rotation of queries and keys: rows in at strides between tokens (in values), results as [batch, heads, tokens, D] or,
+// K and V appended, as codes at slots[b] + i of caches of kv_len tokens (slots, caches) in the place of k_out and v_out.
+struct RopeArgs {
+    const void *q, *k, *v;
+    long q_stride, k_stride, v_stride;
+    const void *q_weight, *k_weight;   // bf16 [D], or null: no norm
+    const float* cos_sin;              // [table_len, D]: D/2 cosines, then the sines
+    const int *positions, *slots;      // [batch, seq_len]; [batch]
+    void *q_out, *k_out, *v_out;
+    int8_t* k_codes;
+    float* k_scale;
+    int8_t* v_codes;
+    float* v_scale;
+    int batch, q_heads, kv_heads, seq_len, head_dim, kv_len, table_len;
+    bool interleaved;
+    double eps;
+};
+hipError_t launch_qk_norm_rope(const RopeArgs& a, bool append, hipStream_t stream);
+
 struct PrefillArgs {
     const void* q;
     const void* k;

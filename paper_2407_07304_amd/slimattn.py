@@ -72,6 +72,11 @@ def load():
         lib.slim_attn_decode_int8_plan.restype = i
         lib.slim_attn_decode_int8_plan_options.argtypes = [i, i, i, i, i, i, ctypes.POINTER(i), ctypes.POINTER(i)]
         lib.slim_attn_decode_int8_plan_options.restype = i
+        d, n = ctypes.c_double, ctypes.c_int64
+        lib.slim_qk_norm_rope.argtypes = [p, p, p, n, n, n, p, p, p, p, p, p, p] + [i] * 7 + [d, p]
+        lib.slim_qk_norm_rope.restype = i
+        lib.slim_qk_norm_rope_append_int8.argtypes = [p, p, p, n, n, n, p, p, p, p, p, p, p, p, p, p] + [i] * 8 + [d, p]
+        lib.slim_qk_norm_rope_append_int8.restype = i
         lib.slim_status_string.argtypes = [i]
         lib.slim_status_string.restype = ctypes.c_char_p
         _lib = lib
@@ -168,3 +173,28 @@ def slim_attn_prefill_strip_max_seq_len() -> int:
 def slim_attn_prefill_strip(q, k, v, softmax_scale, causal=True, out=None, out_dtype=torch.bfloat16):
     """The comparison variant of the bf16 prefill that keeps a row block's whole score strip on chip."""
     return (_native or _load_native()).prefill_strip(q, k, v, softmax_scale, causal, out, out_dtype)
+
+
+def slim_rope_table(length, head_dim, base=10000.0, device="cuda"):
+    """The cosines, then the sines, of position x base^(-2i / head_dim): fp32 [length, head_dim], the angles in 64 bits.
+    (Any other table of this layout will do for the two calls below: scaled frequencies are the caller's affair.)"""
+    inverse = float(base) ** (-torch.arange(0, head_dim, 2, dtype=torch.float64) / head_dim)
+    angle = torch.arange(length, dtype=torch.float64)[:, None] * inverse
+    return torch.cat([angle.cos(), angle.sin()], 1).float().to(device)
+
+
+def slim_qk_norm_rope(q, k, v, cos_sin, positions, q_weight=None, k_weight=None, eps=1e-6, interleaved=False, q_out=None,
+                      k_out=None, v_out=None):
+    """q [B,S,Hq,D], k, v [B,S,Hkv,D] bf16, tokens at any stride (slices of one projection's output) -> normed and rotated
+    q [B,Hq,S,D], k [B,Hkv,S,D] and v [B,Hkv,S,D] bf16; cos_sin fp32 [table length, D], positions int32 [B,S] (-1: padding,
+    rows of zeros), weights bf16 [D] or None (no norm)."""
+    return (_native or _load_native()).qk_norm_rope(q, k, v, cos_sin, positions, q_weight, k_weight, eps, interleaved, q_out,
+                                                    k_out, v_out)
+
+
+def slim_qk_norm_rope_append_int8(q, k, v, cos_sin, positions, slots, k_codes, k_scale, v_codes, v_scale, q_weight=None,
+                                  k_weight=None, eps=1e-6, interleaved=False, q_out=None):
+    """slim_qk_norm_rope with K and V quantised into tokens slots[b] + s of the cache (codes [B,Hkv,T,D] int8, scales
+    [B,Hkv,T] fp32, updated in place; slots int32 [B] on the device) -> q [B,Hq,S,D] bf16."""
+    return (_native or _load_native()).qk_norm_rope_append(q, k, v, cos_sin, positions, slots, k_codes, k_scale, v_codes, v_scale,
+                                                           q_weight, k_weight, eps, interleaved, q_out)

@@ -294,6 +294,32 @@ int slim_qk_norm_rope_append_int8(const void* q_bf16, const void* k_bf16, const 
                                   int batch, int q_heads, int kv_heads, int seq_len, int kv_len, int head_dim, int table_len,
                                   int interleaved, double eps, void* stream);
 
+/*
+ * Decode attention of a batch whose sequences share a long prefix (a system prompt, one document with many questions): the
+ * prefix's tokens are cached once for all of them, and every sequence has a cache of its own for what follows:
+ *     s_t over the prefix's prefix_len tokens and then the sequence's first kv_lens[b] own tokens, as in slim_attn_decode_int8
+ *     o[b,h,:] = sum_t softmax_t(s) * v^_t
+ * one softmax over both parts.  The prefix is read once for up to 128 query rows (batch x query heads of a KV head) and its
+ * products run on the matrix cores; probabilities times v_scale are rounded to bf16 before the second product.
+ * q_bf16    device, in   [batch, q_heads, 1, head_dim] bf16
+ * prefix_k_codes, prefix_v_codes  device, in  [kv_heads, prefix_len, head_dim] int8 (what slim_attn_prefill_emit_int8 writes for a
+ *           batch of one);  prefix_k_scale, prefix_v_scale  [kv_heads, prefix_len] fp32
+ * k_codes, v_codes  device, in  [batch, kv_heads, kv_len, head_dim] int8;  k_scale, v_scale  [batch, kv_heads, kv_len] fp32
+ * kv_lens   device, in   [batch] int32, 4-byte aligned: 0 (the prefix alone) to kv_len; a value outside is taken as the nearest bound
+ * out_bf16  device, out  [batch, q_heads, 1, head_dim] bf16
+ * workspace device, scratch, at least slim_attn_decode_int8_shared_prefix_workspace_bytes(...) bytes (0: the shape is invalid);
+ *           contents before and after the call are meaningless; calls that may run at the same time need one each.
+ * What lies past a sequence's length is never read into the result.  batch x kv_heads x splits, and batch x q_heads, must stay
+ * below 2^24 (SLIM_ERR_SHAPE).  The result does not depend on the order in which workgroups finish.
+ */
+size_t slim_attn_decode_int8_shared_prefix_workspace_bytes(int batch, int q_heads, int kv_heads, int prefix_len, int kv_len, int head_dim);
+int slim_attn_decode_int8_shared_prefix(const void* q_bf16, const int8_t* prefix_k_codes, const float* prefix_k_scale,
+                                        const int8_t* prefix_v_codes, const float* prefix_v_scale,
+                                        const int8_t* k_codes, const float* k_scale, const int8_t* v_codes, const float* v_scale,
+                                        const int32_t* kv_lens, void* out_bf16, void* workspace, size_t workspace_bytes,
+                                        int batch, int q_heads, int kv_heads, int prefix_len, int kv_len, int head_dim,
+                                        int causal, float softmax_scale, void* stream);
+
 /* Name of a status code; pointer to static storage, never NULL. */
 const char* slim_status_string(int status);
 

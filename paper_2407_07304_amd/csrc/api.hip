@@ -413,4 +413,41 @@ int slim_qk_norm_rope_append_int8(const void* q_bf16, const void* k_bf16, const 
     return rope_common(a, true, (hipStream_t)stream);
 }
 
+size_t slim_attn_decode_int8_shared_prefix_workspace_bytes(int batch, int q_heads, int kv_heads, int prefix_len, int kv_len, int head_dim) {
+    if (check_shape(batch, q_heads, kv_heads, kv_len, head_dim) != SLIM_OK || check_shape(1, q_heads, kv_heads, prefix_len, head_dim) != SLIM_OK)
+        return 0;
+    if (!slim::decode_prefix_fits(batch, q_heads, kv_heads, prefix_len, kv_len, head_dim)) return 0;
+    return slim::decode_prefix_workspace_bytes(batch, q_heads, kv_heads, prefix_len, kv_len, head_dim);
+}
+
+int slim_attn_decode_int8_shared_prefix(const void* q_bf16, const int8_t* prefix_k_codes, const float* prefix_k_scale,
+                                        const int8_t* prefix_v_codes, const float* prefix_v_scale, const int8_t* k_codes,
+                                        const float* k_scale, const int8_t* v_codes, const float* v_scale, const int32_t* kv_lens,
+                                        void* out_bf16, void* workspace, size_t workspace_bytes, int batch, int q_heads, int kv_heads,
+                                        int prefix_len, int kv_len, int head_dim, int causal, float softmax_scale, void* stream) {
+    const void* const all[12] = {q_bf16, prefix_k_codes, prefix_k_scale, prefix_v_codes, prefix_v_scale, k_codes, k_scale,
+                                 v_codes, v_scale, out_bf16, workspace, kv_lens};
+    for (const void* p : all)
+        if (!p) return SLIM_ERR_NULL;
+    int st = check_shape(batch, q_heads, kv_heads, kv_len, head_dim);
+    if (st == SLIM_OK) st = check_shape(1, q_heads, kv_heads, prefix_len, head_dim);
+    if (st != SLIM_OK) return st;
+    if (causal != 0 && causal != 1) return SLIM_ERR_SHAPE;
+    if (!(softmax_scale > 0.0f) || !isfinite(softmax_scale)) return SLIM_ERR_SHAPE;
+    if (!slim::decode_prefix_fits(batch, q_heads, kv_heads, prefix_len, kv_len, head_dim)) return SLIM_ERR_SHAPE;
+    for (int i = 0; i < 11; ++i)
+        if (misaligned(all[i])) return SLIM_ERR_ALIGN;
+    if ((uintptr_t)kv_lens & 3u) return SLIM_ERR_ALIGN;
+    if (workspace_bytes < slim::decode_prefix_workspace_bytes(batch, q_heads, kv_heads, prefix_len, kv_len, head_dim)) return SLIM_ERR_WORKSPACE;
+    slim::PrefixArgs a;
+    a.q = q_bf16;
+    a.prefix_k_codes = prefix_k_codes, a.prefix_k_scale = prefix_k_scale, a.prefix_v_codes = prefix_v_codes, a.prefix_v_scale = prefix_v_scale;
+    a.k_codes = k_codes, a.k_scale = k_scale, a.v_codes = v_codes, a.v_scale = v_scale;
+    a.kv_lens = kv_lens, a.out = out_bf16, a.workspace = (float*)workspace;
+    a.batch = batch, a.q_heads = q_heads, a.kv_heads = kv_heads, a.prefix_len = prefix_len, a.kv_len = kv_len, a.head_dim = head_dim;
+    a.softmax_scale = softmax_scale;
+    drop_stale_hip_error();
+    return slim::launch_decode_prefix(a, (hipStream_t)stream) == hipSuccess ? SLIM_OK : SLIM_ERR_LAUNCH;
+}
+
 }  // extern "C"

@@ -471,6 +471,47 @@ PyObject* qk_norm_rope(Args a) {
     }
 }
 
+// q, prefix_k_codes, prefix_k_scale, prefix_v_codes, prefix_v_scale, k_codes, k_scale, v_codes, v_scale, kv_lens, softmax_scale,
+// causal, out, workspace
+PyObject* decode_shared_prefix(Args a) {
+    const at::Tensor& q = tensor(a[0]);
+    const Dims4 n = dims4(q), pre = dims4(tensor(a[1])), own = dims4(tensor(a[5]));
+    require(n.s == 1, "one query token per sequence");
+    require_shape(tensor(a[1]), {1, own.h, pre.s, n.d}, "shape of prefix_k_codes");
+    require_shape(tensor(a[5]), {n.b, own.h, own.s, n.d}, "shape of k_codes");
+    require(tensor(a[3]).sizes() == tensor(a[1]).sizes(), "prefix_k_codes and prefix_v_codes have one shape");
+    require(tensor(a[7]).sizes() == tensor(a[5]).sizes(), "k_codes and v_codes have one shape");
+    require_shape(tensor(a[2]), {1, own.h, pre.s}, "shape of prefix_k_scale");
+    require_shape(tensor(a[4]), {1, own.h, pre.s}, "shape of prefix_v_scale");
+    require_shape(tensor(a[6]), {n.b, own.h, own.s}, "shape of k_scale");
+    require_shape(tensor(a[8]), {n.b, own.h, own.s}, "shape of v_scale");
+    require_shape(tensor(a[9]), {n.b}, "one length per sequence");
+    require_one_device({a[0], a[1], a[2], a[3], a[4], a[5], a[6], a[7], a[8], a[9], a[12], a[13]});
+    void* const qp = bf16_ptr(q);
+    const c10::DeviceGuard guard(q.device());
+    const at::Tensor out = out_or_new(a[12], {n.b, n.h, 1, n.d}, at::kBFloat16, q);
+    require_shape(out, {n.b, n.h, 1, n.d}, "shape of out");
+    const int B = c_int(n.b), Hq = c_int(n.h), Hkv = c_int(own.h), P = c_int(pre.s), T = c_int(own.s), D = c_int(n.d);
+    at::Tensor fresh_ws;
+    if (!given(a[13])) {
+        const size_t need = slim_attn_decode_int8_shared_prefix_workspace_bytes(B, Hq, Hkv, P, T, D);
+        fresh_ws = make({(int64_t)std::max<size_t>(need, 16)}, at::kByte, q);
+    }
+    const at::Tensor& ws = given(a[13]) ? tensor(a[13]) : fresh_ws;
+    const int8_t *const pkc = i8_ptr(tensor(a[1])), *const pvc = i8_ptr(tensor(a[3])), *const kc = i8_ptr(tensor(a[5])), *const vc = i8_ptr(tensor(a[7]));
+    const float *const pks = f32_ptr(tensor(a[2])), *const pvs = f32_ptr(tensor(a[4])), *const ks = f32_ptr(tensor(a[6])), *const vs = f32_ptr(tensor(a[8]));
+    const int32_t* const lens = i32_ptr(tensor(a[9]));
+    void *const op = bf16_ptr(out), *const wp = ptr(ws);
+    const size_t ws_bytes = ws.nbytes();
+    const int causal = as_flag(a[11]);
+    const float scale = as_float(a[10]);
+    call([&](void* stream) {
+        return slim_attn_decode_int8_shared_prefix(qp, pkc, pks, pvc, pvs, kc, ks, vc, vs, lens, op, wp, ws_bytes, B, Hq, Hkv, P, T, D, causal,
+                                                   scale, stream);
+    });
+    return give(a[12], out);
+}
+
 template <PyObject* (*F)(Args), int N>
 PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
     if (n != N) {
@@ -506,6 +547,7 @@ PyMethodDef g_methods[] = {
     SLIM_ENTRY("decode_static", decode_static, 8),
     SLIM_ENTRY("qk_norm_rope", qk_norm_rope<false>, 12),
     SLIM_ENTRY("qk_norm_rope_append", qk_norm_rope<true>, 15),
+    SLIM_ENTRY("decode_shared_prefix", decode_shared_prefix, 14),
     {"set_raise_status", set_raise_status, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_slimbind", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};

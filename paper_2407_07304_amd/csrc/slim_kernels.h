@@ -108,4 +108,26 @@ inline size_t decode_records_bytes(long n_rows, int n_split, int head_dim) {
     return (size_t)n_rows * n_split * ((size_t)head_dim + 2) * sizeof(float);
 }
 
+// Decode of a batch behind a shared prefix: the prefix's cache [1, kv_heads, prefix_len, D], the sequences' own [batch, kv_heads,
+// kv_len, D] of which kv_lens[b] (clamped to 0..kv_len) tokens count.
+struct PrefixArgs {
+    const void* q;
+    const int8_t* prefix_k_codes;
+    const float* prefix_k_scale;
+    const int8_t* prefix_v_codes;
+    const float* prefix_v_scale;
+    const int8_t* k_codes;
+    const float* k_scale;
+    const int8_t* v_codes;
+    const float* v_scale;
+    const int* kv_lens;
+    void* out;
+    float* workspace;
+    int batch, q_heads, kv_heads, prefix_len, kv_len, head_dim;
+    float softmax_scale;
+};
+bool decode_prefix_fits(int batch, int q_heads, int kv_heads, int prefix_len, int kv_len, int head_dim);   // in a launch
+size_t decode_prefix_workspace_bytes(int batch, int q_heads, int kv_heads, int prefix_len, int kv_len, int head_dim);
+hipError_t launch_decode_prefix(const PrefixArgs& a, hipStream_t stream);
+
 }  // namespace slim

@@ -77,6 +77,10 @@ def load():
         lib.slim_qk_norm_rope.restype = i
         lib.slim_qk_norm_rope_append_int8.argtypes = [p, p, p, n, n, n, p, p, p, p, p, p, p, p, p, p] + [i] * 8 + [d, p]
         lib.slim_qk_norm_rope_append_int8.restype = i
+        lib.slim_attn_decode_int8_shared_prefix_workspace_bytes.argtypes = [i] * 6
+        lib.slim_attn_decode_int8_shared_prefix_workspace_bytes.restype = ctypes.c_size_t
+        lib.slim_attn_decode_int8_shared_prefix.argtypes = [p] * 12 + [ctypes.c_size_t] + [i] * 7 + [f, p]
+        lib.slim_attn_decode_int8_shared_prefix.restype = i
         lib.slim_status_string.argtypes = [i]
         lib.slim_status_string.restype = ctypes.c_char_p
         _lib = lib
@@ -198,3 +202,15 @@ def slim_qk_norm_rope_append_int8(q, k, v, cos_sin, positions, slots, k_codes, k
     [B,Hkv,T] fp32, updated in place; slots int32 [B] on the device) -> q [B,Hq,S,D] bf16."""
     return (_native or _load_native()).qk_norm_rope_append(q, k, v, cos_sin, positions, slots, k_codes, k_scale, v_codes, v_scale,
                                                            q_weight, k_weight, eps, interleaved, q_out)
+
+
+def slim_attn_decode_int8_shared_prefix_workspace_bytes(batch, q_heads, kv_heads, prefix_len, kv_len, head_dim) -> int:
+    return int(load().slim_attn_decode_int8_shared_prefix_workspace_bytes(batch, q_heads, kv_heads, prefix_len, kv_len, head_dim))
+
+
+def slim_attn_decode_int8_shared_prefix(q, prefix_k_codes, prefix_k_scale, prefix_v_codes, prefix_v_scale, k_codes, k_scale,
+                                        v_codes, v_scale, kv_lens, softmax_scale, causal=False, out=None, workspace=None):
+    """slim_attn_decode_int8_varlen behind a prefix that all sequences share: its cache has codes [1,Hkv,P,D] int8 and scales
+    [1,Hkv,P] fp32, the sequences' own follows as in slim_attn_decode_int8_varlen; kv_lens [B] int32 may be 0."""
+    return (_native or _load_native()).decode_shared_prefix(q, prefix_k_codes, prefix_k_scale, prefix_v_codes, prefix_v_scale, k_codes,
+                                                            k_scale, v_codes, v_scale, kv_lens, softmax_scale, causal, out, workspace)

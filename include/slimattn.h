@@ -320,6 +320,46 @@ int slim_attn_decode_int8_shared_prefix(const void* q_bf16, const int8_t* prefix
                                         int batch, int q_heads, int kv_heads, int prefix_len, int kv_len, int head_dim,
                                         int causal, float softmax_scale, void* stream);
 
+/*
+ * slim_attn_decode_int8_varlen that also gives the attention weight of every cached token, summed over the query heads of its KV
+ * head: what slim_cache_evict_int8 goes by.
+ *     weights_out[b,g,t] = weights_in[b,g,t] + sum_{h reads g} softmax_t(s[b,h,:])     for t < kv_lens[b], and 0 past it
+ * The weights are fp32, of the unrounded probabilities.  (A token that is appended later thus starts at 0.)
+ * weights_in   device, in   [batch, kv_heads, kv_len] fp32, or NULL (zeros)
+ * weights_out  device, out  [batch, kv_heads, kv_len] fp32; may be weights_in: the sums over the steps of a sequence
+ * workspace    device, scratch, at least slim_attn_decode_int8_weights_workspace_bytes(...) bytes (0: the shape is invalid): every
+ *              score in fp32, and the splits' records; calls that may run at the same time need one each.
+ * kv_lens is taken as in slim_attn_decode_int8_varlen (1 to kv_len); weights_out must not overlap any buffer but weights_in, and
+ * that only if it is the same (SLIM_ERR_OVERLAP).  batch x kv_heads x splits must stay below 2^23 (SLIM_ERR_SHAPE).
+ */
+size_t slim_attn_decode_int8_weights_workspace_bytes(int batch, int q_heads, int kv_heads, int kv_len, int head_dim);
+int slim_attn_decode_int8_weights(const void* q_bf16, const int8_t* k_codes, const float* k_scale,
+                                  const int8_t* v_codes, const float* v_scale, const int32_t* kv_lens,
+                                  const float* weights_in, float* weights_out, void* out_bf16, void* workspace, size_t workspace_bytes,
+                                  int batch, int q_heads, int kv_heads, int kv_len, int head_dim,
+                                  int causal, float softmax_scale, void* stream);
+
+/*
+ * Eviction: cuts every sequence's cache down to at most `keep` tokens a KV head.  Of the first kv_lens[b] tokens of (b, g) the
+ * `recent` last ones stay, and of the others the keep - recent of largest weight (equal weights: the lower index; NaN counts as
+ * the smallest).  They are copied, in their order, to the first places of another cache; a sequence of at most `keep` tokens keeps
+ * them all.  Codes and scales are moved as they are; no position is part of them.
+ * k_codes, v_codes, k_scale, v_scale  device, in  [batch, kv_heads, kv_len, head_dim] int8, [batch, kv_heads, kv_len] fp32
+ * weights      device, in   [batch, kv_heads, kv_len] fp32
+ * kv_lens      device, in   [batch] int32, 4-byte aligned: 0 to kv_len; a value outside is taken as the nearest bound
+ * ..._out      device, out  the same for a cache of out_len tokens, keep <= out_len; codes and scales past what stays are left as
+ *              they were, weights past it are 0
+ * kept         device, out  [batch, kv_heads, keep] int32: the tokens' former indices, -1 past what stays
+ * kv_lens_out  device, out  [batch] int32: min(kv_lens[b], keep)
+ * 1 <= keep, 0 <= recent <= keep (SLIM_ERR_SHAPE); no result may overlap another buffer (SLIM_ERR_OVERLAP).  batch x kv_heads must
+ * stay below 2^22, and that times out_len / 64 below 2^24 (SLIM_ERR_SHAPE).
+ */
+int slim_cache_evict_int8(const int8_t* k_codes, const float* k_scale, const int8_t* v_codes, const float* v_scale,
+                          const float* weights, const int32_t* kv_lens,
+                          int8_t* k_codes_out, float* k_scale_out, int8_t* v_codes_out, float* v_scale_out, float* weights_out,
+                          int32_t* kept, int32_t* kv_lens_out,
+                          int batch, int kv_heads, int kv_len, int out_len, int head_dim, int keep, int recent, void* stream);
+
 /* Name of a status code; pointer to static storage, never NULL. */
 const char* slim_status_string(int status);
 

@@ -9,7 +9,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libslimattn.so")
 SOURCES = ["api.hip", "kv_quant.hip", "decode.hip", "decode_gqa.hip", "prefill.hip", "prefill_split.hip", "prefill_strip.hip",
-           "rope.hip", "decode_prefix.hip"]
+           "rope.hip", "decode_prefix.hip", "decode_weights.hip", "cache_evict.hip"]
 PROBE_LIB = os.path.join(HERE, "libslimprobe.so")
 PROBE_SOURCES = ["probes.hip", "decode_gqa.hip"]   # (the grouped-query decode kernel has a traffic-only form)
 # prefill.hip: MFMA results stay in arch VGPRs (no AGPR copies around the softmax), and fmaxf needs no
@@ -19,6 +19,7 @@ EXTRA = {"prefill.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form", "-fno-honor-nans", 
          "prefill_strip.hip": ["-fno-honor-nans"],
          "prefill_split.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form", "-fno-honor-nans"],
          "decode_prefix.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form", "-fno-honor-nans"],
+         "decode_weights.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form", "-fno-honor-nans"],
          "decode_gqa.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form", "-fno-honor-nans"]}
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 

@@ -450,4 +450,76 @@ int slim_attn_decode_int8_shared_prefix(const void* q_bf16, const int8_t* prefix
     return slim::launch_decode_prefix(a, (hipStream_t)stream) == hipSuccess ? SLIM_OK : SLIM_ERR_LAUNCH;
 }
 
+size_t slim_attn_decode_int8_weights_workspace_bytes(int batch, int q_heads, int kv_heads, int kv_len, int head_dim) {
+    if (check_shape(batch, q_heads, kv_heads, kv_len, head_dim) != SLIM_OK) return 0;
+    if (!slim::decode_weights_fits(batch, q_heads, kv_heads, kv_len, head_dim)) return 0;
+    return slim::decode_weights_workspace_bytes(batch, q_heads, kv_heads, kv_len, head_dim);
+}
+
+int slim_attn_decode_int8_weights(const void* q_bf16, const int8_t* k_codes, const float* k_scale, const int8_t* v_codes,
+                                  const float* v_scale, const int32_t* kv_lens, const float* weights_in, float* weights_out,
+                                  void* out_bf16, void* workspace, size_t workspace_bytes, int batch, int q_heads, int kv_heads,
+                                  int kv_len, int head_dim, int causal, float softmax_scale, void* stream) {
+    if (!q_bf16 || !k_codes || !k_scale || !v_codes || !v_scale || !kv_lens || !weights_out || !out_bf16 || !workspace) return SLIM_ERR_NULL;
+    const int st = check_shape(batch, q_heads, kv_heads, kv_len, head_dim);
+    if (st != SLIM_OK) return st;
+    if (causal != 0 && causal != 1) return SLIM_ERR_SHAPE;
+    if (!(softmax_scale > 0.0f) || !isfinite(softmax_scale)) return SLIM_ERR_SHAPE;
+    if (!slim::decode_weights_fits(batch, q_heads, kv_heads, kv_len, head_dim)) return SLIM_ERR_SHAPE;
+    if (misaligned(q_bf16) || misaligned(k_codes) || misaligned(k_scale) || misaligned(v_codes) || misaligned(v_scale) ||
+        misaligned(weights_in) || misaligned(weights_out) || misaligned(out_bf16) || misaligned(workspace))
+        return SLIM_ERR_ALIGN;
+    if ((uintptr_t)kv_lens & 3u) return SLIM_ERR_ALIGN;
+    const size_t need = slim::decode_weights_workspace_bytes(batch, q_heads, kv_heads, kv_len, head_dim);
+    if (workspace_bytes < need) return SLIM_ERR_WORKSPACE;
+    const size_t rows = (size_t)batch * kv_heads * kv_len, q_bytes = (size_t)batch * q_heads * head_dim * 2;
+    const bool other_in = weights_in && weights_in != weights_out;
+    const Range r[10] = {{weights_out, rows * 4}, {out_bf16, q_bytes}, {workspace, need}, {q_bf16, q_bytes}, {k_codes, rows * head_dim},
+                         {v_codes, rows * head_dim}, {k_scale, rows * 4}, {v_scale, rows * 4}, {kv_lens, (size_t)batch * 4},
+                         {weights_in, other_in ? rows * 4 : 0}};
+    if (any_overlap(r, 3, other_in ? 10 : 9)) return SLIM_ERR_OVERLAP;
+    slim::DecodeArgs a;
+    a.q = q_bf16;
+    a.k_codes = k_codes, a.k_scale = k_scale, a.v_codes = v_codes, a.v_scale = v_scale;
+    a.out = out_bf16, a.workspace = (float*)workspace, a.kv_lens = kv_lens;
+    a.batch = batch, a.q_heads = q_heads, a.kv_heads = kv_heads, a.kv_len = kv_len, a.head_dim = head_dim;
+    a.softmax_scale = softmax_scale;
+    a.ragged = true;
+    drop_stale_hip_error();
+    return slim::launch_decode_weights(a, weights_in, weights_out, (hipStream_t)stream) == hipSuccess ? SLIM_OK : SLIM_ERR_LAUNCH;
+}
+
+int slim_cache_evict_int8(const int8_t* k_codes, const float* k_scale, const int8_t* v_codes, const float* v_scale,
+                          const float* weights, const int32_t* kv_lens, int8_t* k_codes_out, float* k_scale_out, int8_t* v_codes_out,
+                          float* v_scale_out, float* weights_out, int32_t* kept, int32_t* kv_lens_out, int batch, int kv_heads,
+                          int kv_len, int out_len, int head_dim, int keep, int recent, void* stream) {
+    const void* const all[13] = {k_codes, k_scale, v_codes, v_scale, weights, k_codes_out, k_scale_out, v_codes_out, v_scale_out,
+                                 weights_out, kv_lens, kept, kv_lens_out};
+    for (const void* p : all)
+        if (!p) return SLIM_ERR_NULL;
+    int st = check_shape(batch, kv_heads, kv_heads, kv_len, head_dim);
+    if (st == SLIM_OK) st = check_shape(batch, kv_heads, kv_heads, out_len, head_dim);
+    if (st != SLIM_OK) return st;
+    if (keep < 1 || keep > out_len || recent < 0 || recent > keep) return SLIM_ERR_SHAPE;
+    const long bg = (long)batch * kv_heads;   // (a launch has less than 2^32 threads)
+    if (bg >= (1L << 22) || bg * ((out_len + 63) / 64) >= (1L << 24)) return SLIM_ERR_SHAPE;
+    for (int i = 0; i < 10; ++i)
+        if (misaligned(all[i])) return SLIM_ERR_ALIGN;
+    for (int i = 10; i < 13; ++i)
+        if ((uintptr_t)all[i] & 3u) return SLIM_ERR_ALIGN;
+    const size_t in = (size_t)bg * kv_len, out = (size_t)bg * out_len;
+    const Range r[13] = {{k_codes_out, out * head_dim}, {k_scale_out, out * 4}, {v_codes_out, out * head_dim}, {v_scale_out, out * 4},
+                         {weights_out, out * 4}, {kept, (size_t)bg * keep * 4}, {kv_lens_out, (size_t)batch * 4},
+                         {k_codes, in * head_dim}, {k_scale, in * 4}, {v_codes, in * head_dim}, {v_scale, in * 4}, {weights, in * 4},
+                         {kv_lens, (size_t)batch * 4}};
+    if (any_overlap(r, 7, 13)) return SLIM_ERR_OVERLAP;
+    slim::EvictArgs a;
+    a.k_codes = k_codes, a.k_scale = k_scale, a.v_codes = v_codes, a.v_scale = v_scale, a.weights = weights, a.kv_lens = kv_lens;
+    a.k_codes_out = k_codes_out, a.k_scale_out = k_scale_out, a.v_codes_out = v_codes_out, a.v_scale_out = v_scale_out;
+    a.weights_out = weights_out, a.kept = kept, a.kv_lens_out = kv_lens_out;
+    a.batch = batch, a.kv_heads = kv_heads, a.kv_len = kv_len, a.head_dim = head_dim, a.keep = keep, a.recent = recent, a.out_len = out_len;
+    drop_stale_hip_error();
+    return slim::launch_cache_evict(a, (hipStream_t)stream) == hipSuccess ? SLIM_OK : SLIM_ERR_LAUNCH;
+}
+
 }  // extern "C"

@@ -512,6 +512,87 @@ PyObject* decode_shared_prefix(Args a) {
     return give(a[12], out);
 }
 
+// q, k_codes, k_scale, v_codes, v_scale, kv_lens, softmax_scale, weights_in, weights_out, causal, out, workspace
+PyObject* decode_weights(Args a) {
+    DecodeIn in(a);
+    const at::Tensor& q = tensor(a[0]);
+    require_shape(tensor(a[5]), {in.b}, "one length per sequence");
+    if (given(a[7])) require_shape(tensor(a[7]), {in.b, in.hkv, in.t}, "shape of weights_in");
+    require_one_device({a[0], a[1], a[2], a[3], a[4], a[5], a[7], a[8], a[10], a[11]});
+    in.take_pointers(a);
+    const c10::DeviceGuard guard(q.device());
+    const at::Tensor out = out_or_new(a[10], {in.b, in.hq, 1, in.d}, at::kBFloat16, q);
+    require_shape(out, {in.b, in.hq, 1, in.d}, "shape of out");
+    const at::Tensor weights = out_or_new(a[8], {in.b, in.hkv, in.t}, at::kFloat, q);
+    require_shape(weights, {in.b, in.hkv, in.t}, "shape of weights_out");
+    const int B = c_int(in.b), Hq = c_int(in.hq), Hkv = c_int(in.hkv), T = c_int(in.t), D = c_int(in.d);
+    at::Tensor fresh_ws;
+    if (!given(a[11])) {
+        const size_t need = slim_attn_decode_int8_weights_workspace_bytes(B, Hq, Hkv, T, D);
+        fresh_ws = make({(int64_t)std::max<size_t>(need, 16)}, at::kByte, q);
+    }
+    const at::Tensor& ws = given(a[11]) ? tensor(a[11]) : fresh_ws;
+    const int32_t* const lens = i32_ptr(tensor(a[5]));
+    const float* const wi = given(a[7]) ? f32_ptr(tensor(a[7])) : nullptr;
+    float* const wo = f32_ptr(weights);
+    void *const op = bf16_ptr(out), *const wp = ptr(ws);
+    const size_t ws_bytes = ws.nbytes();
+    const int causal = as_flag(a[9]);
+    const float scale = as_float(a[6]);
+    call([&](void* stream) {
+        return slim_attn_decode_int8_weights(in.q, in.kc, in.ks, in.vc, in.vs, lens, wi, wo, op, wp, ws_bytes, B, Hq, Hkv, T, D, causal, scale,
+                                             stream);
+    });
+    PyObject* items[2] = {give(a[10], out), give(a[8], weights)};
+    return tuple_of(items);
+}
+
+int64_t as_int(PyObject* o) {
+    const long long v = PyLong_AsLongLong(o);
+    if (v == -1 && PyErr_Occurred()) throw Failed();
+    return (int64_t)v;
+}
+
+// k_codes, k_scale, v_codes, v_scale, weights, kv_lens, keep, recent, and the results: k_codes, k_scale, v_codes, v_scale, weights,
+// kept, kv_lens
+PyObject* cache_evict(Args a) {
+    const at::Tensor &kc = tensor(a[0]), &ks = tensor(a[1]), &vc = tensor(a[2]), &vs = tensor(a[3]), &weights = tensor(a[4]), &lens = tensor(a[5]);
+    const Dims4 n = dims4(kc);
+    require(vc.sizes() == kc.sizes(), "k_codes and v_codes have one shape");
+    require_shape(ks, {n.b, n.h, n.s}, "shape of k_scale");
+    require_shape(vs, {n.b, n.h, n.s}, "shape of v_scale");
+    require_shape(weights, {n.b, n.h, n.s}, "shape of weights");
+    require_shape(lens, {n.b}, "one length per sequence");
+    const int64_t keep = as_int(a[6]), recent = as_int(a[7]);
+    if (keep < 1 || keep > 0x7fffffff || recent < 0 || recent > keep) fail(PyExc_ValueError, "1 <= keep, 0 <= recent <= keep");
+    require_one_device({a[0], a[1], a[2], a[3], a[4], a[5], a[8], a[9], a[10], a[11], a[12], a[13], a[14]});
+    const int8_t *const kcp = i8_ptr(kc), *const vcp = i8_ptr(vc);
+    const float *const ksp = f32_ptr(ks), *const vsp = f32_ptr(vs), *const wp = f32_ptr(weights);
+    const int32_t* const lp = i32_ptr(lens);
+    const c10::DeviceGuard guard(kc.device());
+    const int64_t len = given(a[8]) ? dims4(tensor(a[8])).s : keep;   // of the other cache
+    const at::Tensor kc2 = out_or_new(a[8], {n.b, n.h, len, n.d}, at::kChar, kc), ks2 = out_or_new(a[9], {n.b, n.h, len}, at::kFloat, kc);
+    const at::Tensor vc2 = out_or_new(a[10], {n.b, n.h, len, n.d}, at::kChar, kc), vs2 = out_or_new(a[11], {n.b, n.h, len}, at::kFloat, kc);
+    const at::Tensor w2 = out_or_new(a[12], {n.b, n.h, len}, at::kFloat, kc), kept = out_or_new(a[13], {n.b, n.h, keep}, at::kInt, kc);
+    const at::Tensor lens2 = out_or_new(a[14], {n.b}, at::kInt, kc);
+    require_shape(kc2, {n.b, n.h, len, n.d}, "shape of k_codes_out");
+    require_shape(vc2, {n.b, n.h, len, n.d}, "shape of v_codes_out");
+    require_shape(ks2, {n.b, n.h, len}, "shape of k_scale_out");
+    require_shape(vs2, {n.b, n.h, len}, "shape of v_scale_out");
+    require_shape(w2, {n.b, n.h, len}, "shape of weights_out");
+    require_shape(kept, {n.b, n.h, keep}, "shape of kept");
+    require_shape(lens2, {n.b}, "shape of kv_lens_out");
+    int8_t *const kc2p = i8_ptr(kc2), *const vc2p = i8_ptr(vc2);
+    float *const ks2p = f32_ptr(ks2), *const vs2p = f32_ptr(vs2), *const w2p = f32_ptr(w2);
+    int32_t *const kp = i32_ptr(kept), *const l2p = i32_ptr(lens2);
+    call([&](void* stream) {
+        return slim_cache_evict_int8(kcp, ksp, vcp, vsp, wp, lp, kc2p, ks2p, vc2p, vs2p, w2p, kp, l2p, c_int(n.b), c_int(n.h), c_int(n.s), c_int(len),
+                                     c_int(n.d), c_int(keep), c_int(recent), stream);
+    });
+    PyObject* items[7] = {give(a[8], kc2), give(a[9], ks2), give(a[10], vc2), give(a[11], vs2), give(a[12], w2), give(a[13], kept), give(a[14], lens2)};
+    return tuple_of(items);
+}
+
 template <PyObject* (*F)(Args), int N>
 PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
     if (n != N) {
@@ -548,6 +629,8 @@ PyMethodDef g_methods[] = {
     SLIM_ENTRY("qk_norm_rope", qk_norm_rope<false>, 12),
     SLIM_ENTRY("qk_norm_rope_append", qk_norm_rope<true>, 15),
     SLIM_ENTRY("decode_shared_prefix", decode_shared_prefix, 14),
+    SLIM_ENTRY("decode_weights", decode_weights, 12),
+    SLIM_ENTRY("cache_evict", cache_evict, 15),
     {"set_raise_status", set_raise_status, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_slimbind", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};

@@ -411,6 +411,10 @@ DecodePlan decode_plan_of(bool ragged, int batch, int q_heads, int kv_heads, int
     return ragged ? ragged_plan(plan, gqa, batch, q_heads, kv_heads, kv_len, head_dim) : plan;
 }
 
+DecodePlan decode_grouped_plan(int batch, int q_heads, int kv_heads, int kv_len, int head_dim) {
+    return ragged_plan(decode_gqa_plan(kv_len, (long)batch * kv_heads, q_heads / kv_heads, head_dim), true, batch, q_heads, kv_heads, kv_len, head_dim);
+}
+
 bool decode_uses_gqa_kernel(int q_heads, int kv_heads) {
     const int G = q_heads / kv_heads;
     return G >= 2 && G <= 32;

@@ -97,6 +97,8 @@ hipError_t launch_decode_gqa_split(const DecodeArgs& a, float* ws_acc, float* ws
                                    bool traffic_only = false);
 // The plan of a call; ragged: the sequences have lengths of their own
 DecodePlan decode_plan_of(bool ragged, int batch, int q_heads, int kv_heads, int kv_len, int head_dim);
+// The grouped kernel's, lengths of their own, whatever the number of query heads a KV head
+DecodePlan decode_grouped_plan(int batch, int q_heads, int kv_heads, int kv_len, int head_dim);
 size_t decode_workspace_bytes(int batch, int q_heads, int kv_heads, int kv_len, int head_dim, bool ragged);
 hipError_t launch_decode(const DecodeArgs& a, hipStream_t stream);
 // The library's own decode scratch (one static device array per GPU) for the entry point that may not
@@ -129,5 +131,28 @@ struct PrefixArgs {
 bool decode_prefix_fits(int batch, int q_heads, int kv_heads, int prefix_len, int kv_len, int head_dim);   // in a launch
 size_t decode_prefix_workspace_bytes(int batch, int q_heads, int kv_heads, int prefix_len, int kv_len, int head_dim);
 hipError_t launch_decode_prefix(const PrefixArgs& a, hipStream_t stream);
+
+// Decode that also gives the tokens' weights: w_out = w_in (or null: zero) + the sum over a KV head's query heads
+bool decode_weights_fits(int batch, int q_heads, int kv_heads, int kv_len, int head_dim);   // in a launch
+size_t decode_weights_workspace_bytes(int batch, int q_heads, int kv_heads, int kv_len, int head_dim);
+hipError_t launch_decode_weights(const DecodeArgs& a, const float* w_in, float* w_out, hipStream_t stream);
+
+// Of each (sequence, KV head)'s tokens the `recent` last and the keep - recent others of largest weight to another cache
+struct EvictArgs {
+    const int8_t* k_codes;
+    const float* k_scale;
+    const int8_t* v_codes;
+    const float* v_scale;
+    const float* weights;
+    const int* kv_lens;
+    int8_t* k_codes_out;
+    float* k_scale_out;
+    int8_t* v_codes_out;
+    float* v_scale_out;
+    float* weights_out;
+    int *kept, *kv_lens_out;
+    int batch, kv_heads, kv_len, head_dim, keep, recent, out_len;
+};
+hipError_t launch_cache_evict(const EvictArgs& a, hipStream_t stream);
 
 }  // namespace slim

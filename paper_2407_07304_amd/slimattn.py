@@ -81,6 +81,12 @@ def load():
         lib.slim_attn_decode_int8_shared_prefix_workspace_bytes.restype = ctypes.c_size_t
         lib.slim_attn_decode_int8_shared_prefix.argtypes = [p] * 12 + [ctypes.c_size_t] + [i] * 7 + [f, p]
         lib.slim_attn_decode_int8_shared_prefix.restype = i
+        lib.slim_attn_decode_int8_weights_workspace_bytes.argtypes = [i] * 5
+        lib.slim_attn_decode_int8_weights_workspace_bytes.restype = ctypes.c_size_t
+        lib.slim_attn_decode_int8_weights.argtypes = [p] * 10 + [ctypes.c_size_t] + [i] * 6 + [f, p]
+        lib.slim_attn_decode_int8_weights.restype = i
+        lib.slim_cache_evict_int8.argtypes = [p] * 13 + [i] * 7 + [p]
+        lib.slim_cache_evict_int8.restype = i
         lib.slim_status_string.argtypes = [i]
         lib.slim_status_string.restype = ctypes.c_char_p
         _lib = lib
@@ -214,3 +220,25 @@ def slim_attn_decode_int8_shared_prefix(q, prefix_k_codes, prefix_k_scale, prefi
     [1,Hkv,P] fp32, the sequences' own follows as in slim_attn_decode_int8_varlen; kv_lens [B] int32 may be 0."""
     return (_native or _load_native()).decode_shared_prefix(q, prefix_k_codes, prefix_k_scale, prefix_v_codes, prefix_v_scale, k_codes,
                                                             k_scale, v_codes, v_scale, kv_lens, softmax_scale, causal, out, workspace)
+
+
+def slim_attn_decode_int8_weights_workspace_bytes(batch, q_heads, kv_heads, kv_len, head_dim) -> int:
+    return int(load().slim_attn_decode_int8_weights_workspace_bytes(batch, q_heads, kv_heads, kv_len, head_dim))
+
+
+def slim_attn_decode_int8_weights(q, k_codes, k_scale, v_codes, v_scale, kv_lens, softmax_scale, weights_in=None, weights_out=None,
+                                  causal=False, out=None, workspace=None):
+    """slim_attn_decode_int8_varlen that also gives the cached tokens' attention weights -> (out, weights_out): weights_out fp32
+    [B,Hkv,T] is weights_in (or zero) plus the sum of the token's probabilities over the query heads of its KV head, and zero past
+    a sequence's length; weights_out may be weights_in."""
+    return (_native or _load_native()).decode_weights(q, k_codes, k_scale, v_codes, v_scale, kv_lens, softmax_scale, weights_in,
+                                                      weights_out, causal, out, workspace)
+
+
+def slim_cache_evict_int8(k_codes, k_scale, v_codes, v_scale, weights, kv_lens, keep, recent=0, k_codes_out=None, k_scale_out=None,
+                          v_codes_out=None, v_scale_out=None, weights_out=None, kept=None, kv_lens_out=None):
+    """Of every (sequence, KV head)'s first kv_lens[b] tokens the `recent` last and, of the others, those of largest weight, `keep` in
+    all, copied in their order to another cache (of `keep` tokens where none is passed) -> (k_codes_out, k_scale_out, v_codes_out,
+    v_scale_out, weights_out, kept int32 [B,Hkv,keep] with -1 past what stays, kv_lens_out)."""
+    return (_native or _load_native()).cache_evict(k_codes, k_scale, v_codes, v_scale, weights, kv_lens, keep, recent, k_codes_out,
+                                                   k_scale_out, v_codes_out, v_scale_out, weights_out, kept, kv_lens_out)

@@ -261,6 +261,17 @@ def test_eviction_of_difficult_weights(sa, kind):
 
 
 @gpu
+@pytest.mark.parametrize("T", [20000, 40001])
+@pytest.mark.parametrize("spread", [1, 1 << 8, 1 << 20, 1 << 21])
+def test_eviction_of_many_near_weights(sa, T, spread):
+    """Weights of one binade, as many steps apart as `spread`: the first digits of tens of thousands are the same."""
+    rng = np.random.default_rng(T + spread)
+    w = (1 + rng.integers(0, spread, (1, 2, T)) * 2.0 ** -23).astype(np.float32)
+    for keep, recent in ((T // 2, 100), (T - 1, 0), (5, 0)):
+        check_evict(sa, rng, 1, 2, 64, T, keep, recent, keep, w, np.array([T], np.int32), "T%d spread%d keep%d" % (T, spread, keep))
+
+
+@gpu
 def test_eviction_replays_from_a_graph(sa):
     rng = np.random.default_rng(12)
     B, Hkv, T, D, keep, recent = 4, 2, 3000, 128, 1000, 64

@@ -5,7 +5,9 @@
 //
 // The softmax's maximum and sum are known at the end of the sweep only, so the sweep of the grouped decode (decode_sweep.h)
 // leaves its scores, fp32, in the workspace: 4 bytes a query head and token beside the 2 (D + 4) of the cache, written once and read
-// once, mostly in the L2.  (K again in the place of the scores would be D bytes and the first product again.)  Where one workgroup has a
+// once.  The writes are what the sweep takes longer for than a plain decode's: 16 sequences, 64 on 8 heads, T=8192 all full 41.9 and 54 us
+// of kernel, 43.4 with the same stores into one small piece of memory; past the L2 or through it they cost as much or more.  (K again
+// in the place of the scores would be D bytes and the first product again.)  Where one workgroup has a
 // whole (sequence, KV head), it turns its own scores into weights as soon as its waves are merged; where several have a part
 // each, a second launch does, beside the merge of their records.  A lone query head a KV head takes this kernel too: 15 of the 16 columns of
 // its products are empty, but the cache's bytes are the same.
@@ -26,19 +28,22 @@ struct WeightsParams {
     const float* w_in;   // null, or [batch, Hkv, T_alloc]; may be w_out
     float* w_out;
     uint16_t* out;
-    float *scores, *ws_acc, *ws_ml;   // scores [batch, Hq, pitch], in log2 units
-    int batch, Hkv, G, T_alloc, pitch, head_groups, n_split, mode;
+    // scores in log2 units, by tile, so that a wave's 16 rows are one piece: [batch, Hkv, tiles, G, 32].  (A row of T each, of T = 8192
+    // tokens, all 16 would go to one memory channel.)
+    float *scores, *ws_acc, *ws_ml;
+    int batch, Hkv, G, T_alloc, tiles, head_groups, n_split, mode;
     unsigned split_rate;
     float scale_log2e;
 };
 
 typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
 
-// Four tokens' weights of `heads` rows of scores, each by its maximum and the inverse of its sum
-__device__ __forceinline__ f32x4 weights_of(const float* scores, int pitch, int heads, const float* top, const float* inverse) {
+// Weights of tokens t to t + 3 by `heads` rows of scores, each by its maximum and the inverse of its sum; G rows a tile
+__device__ __forceinline__ f32x4 weights_of(const float* scores, int t, int G, int heads, const float* top, const float* inverse) {
     f32x4 w = {0.0f, 0.0f, 0.0f, 0.0f};
+    scores += ((long)(t / kGqaTile) * G) * kGqaTile + t % kGqaTile;
     for (int h = 0; h < heads; ++h) {
-        const f32x4 s = *reinterpret_cast<const f32x4*>(scores + (long)h * pitch);
+        const f32x4 s = *reinterpret_cast<const f32x4*>(scores + h * kGqaTile);
         const float m = top[h], f = inverse[h];
 #pragma unroll
         for (int e = 0; e < 4; ++e) w[e] = fmaf(fast_exp2(s[e] - m), f, w[e]);
@@ -84,7 +89,7 @@ __global__ __launch_bounds__(64 * W) void slim_decode_weights_kernel(const Weigh
     int first, end;
     split_span((T + kGqaTile - 1) / kGqaTile, n_used, sp, first, end);
     first += w;
-    float* const scores = p.scores + row0 * p.pitch;
+    float* const scores = p.scores + (((long)b * p.Hkv + g) * p.tiles * p.G + h0) * kGqaTile;
     const int l16 = lane & 15, lq = lane >> 4;
 
     f32x4 o[NC][D / 16];
@@ -92,11 +97,13 @@ __global__ __launch_bounds__(64 * W) void slim_decode_weights_kernel(const Weigh
     gqa_sweep<D, W, NC, false>(kS, lane, [&](int i) { return p.q + (row0 + min(i, heads - 1)) * D; }, p.kc + kvrow0 * D, p.ks + kvrow0,
                                p.vc + kvrow0 * D, p.vs + kvrow0, T, first, first < end ? (end - first + W - 1) / W : 0, p.scale_log2e,
                                [&](int nc, int t0, const float (&u)[8]) {
-                                   if (16 * nc + l16 < heads) {
-                                       f32x4* to = reinterpret_cast<f32x4*>(scores + (long)(16 * nc + l16) * p.pitch + t0 + 4 * lq);
-                                       to[0] = f32x4{u[0], u[1], u[2], u[3]};
-                                       to[4] = f32x4{u[4], u[5], u[6], u[7]};
-                                   }
+                                   // (through a descriptor over the tile's rows: the columns past the last head store nothing, and the store is the
+                                   // same instructions for all, so that the waits for the loads around it are still counted exactly)
+                                   const __amdgpu_buffer_rsrc_t to =
+                                       __builtin_amdgcn_make_buffer_rsrc((void*)(scores + (long)t0 * p.G), 0, heads * (kGqaTile * 4), 0x00020000);
+                                   const int off = (16 * nc + l16) * (kGqaTile * 4) + 16 * lq;
+                                   __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, f32x4{u[0], u[1], u[2], u[3]}), to, off, 0, 0);
+                                   __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, f32x4{u[4], u[5], u[6], u[7]}), to, off + 64, 0, 0);
                                },
                                o, M, lsum);
     gqa_record<D, NC>(kS, lane, o, M, lsum);
@@ -120,7 +127,7 @@ __global__ __launch_bounds__(64 * W) void slim_decode_weights_kernel(const Weigh
         const float* const w_in = p.w_in ? p.w_in + kvrow0 : nullptr;
         for (int t = 4 * threadIdx.x; t < p.T_alloc; t += 256 * W)
             store_weights(w_in, p.w_out + kvrow0, t, T, p.T_alloc,
-                          t < T ? weights_of(scores + t, p.pitch, heads, topS, inverseS) : f32x4{0.0f, 0.0f, 0.0f, 0.0f});
+                          t < T ? weights_of(scores, t, p.G, heads, topS, inverseS) : f32x4{0.0f, 0.0f, 0.0f, 0.0f});
     }
 }
 
@@ -171,7 +178,7 @@ __global__ __launch_bounds__(256) void slim_decode_weights_finish_kernel(const W
                 }
             }
             __syncthreads();
-            if (t < T) sum += weights_of(p.scores + (row0 + h0) * p.pitch + t, p.pitch, heads, topS, inverseS);
+            if (t < T) sum += weights_of(p.scores + ((long)bg * p.tiles * p.G + h0) * kGqaTile, t, p.G, heads, topS, inverseS);
         }
     }
     if (t < p.T_alloc) store_weights(p.w_in ? p.w_in + kvrow0 : nullptr, p.w_out + kvrow0, t, T, p.T_alloc, sum);
@@ -182,12 +189,12 @@ static DecodePlan weights_plan(int batch, int q_heads, int kv_heads, int kv_len,
     const int hg = weights_head_groups(q_heads, kv_heads), group = std::min(q_heads / kv_heads, 32);
     return decode_grouped_plan(batch, kv_heads * hg * group, kv_heads * hg, kv_len, head_dim);
 }
-static long weights_pitch(int kv_len) { return ((long)kv_len + 31) / 32 * 32; }
+static long weights_tiles(int kv_len) { return ((long)kv_len + kGqaTile - 1) / kGqaTile; }
 
 size_t decode_weights_workspace_bytes(int batch, int q_heads, int kv_heads, int kv_len, int head_dim) {
     const long rows = (long)batch * q_heads;
     return decode_records_bytes(rows, weights_plan(batch, q_heads, kv_heads, kv_len, head_dim).n_split, head_dim) +
-           (size_t)rows * weights_pitch(kv_len) * sizeof(float);
+           (size_t)rows * weights_tiles(kv_len) * kGqaTile * sizeof(float);
 }
 
 bool decode_weights_fits(int batch, int q_heads, int kv_heads, int kv_len, int head_dim) {
@@ -206,11 +213,11 @@ hipError_t launch_decode_weights(const DecodeArgs& a, const float* w_in, float* 
     p.kc = a.k_codes, p.ks = a.k_scale, p.vc = a.v_codes, p.vs = a.v_scale;
     p.kv_lens = a.kv_lens, p.w_in = w_in, p.w_out = w_out, p.out = (uint16_t*)a.out;
     p.batch = a.batch, p.Hkv = a.kv_heads, p.G = a.q_heads / a.kv_heads, p.T_alloc = a.kv_len;
-    p.pitch = (int)weights_pitch(a.kv_len);
+    p.tiles = (int)weights_tiles(a.kv_len);
     p.head_groups = weights_head_groups(a.q_heads, a.kv_heads);
     p.n_split = plan.n_split, p.split_rate = plan.split_rate, p.mode = decode_mode(plan, a.batch);
-    p.scores = a.workspace;   // (rows of whole cache lines)
-    p.ws_acc = p.scores + rows * p.pitch;
+    p.scores = a.workspace;
+    p.ws_acc = p.scores + rows * p.tiles * kGqaTile;
     p.ws_ml = p.ws_acc + rows * plan.n_split * a.head_dim;
     p.scale_log2e = a.softmax_scale * kLog2e;
     const bool whole = plan.n_split == 1 && p.head_groups == 1;

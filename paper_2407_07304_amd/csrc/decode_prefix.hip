@@ -24,31 +24,35 @@
 
 namespace slim {
 
-// LDS of the form with shared tiles: two stages of K and V rows (padded so that row reads and transpose reads spread over the
-// banks) and of their scales
-template <int D, int RG>
+// LDS of the form with shared tiles: two stages of 64 tokens' K and V rows (padded so that row reads and transpose reads spread over
+// the banks) and of their scales
+template <int D>
 struct PrefixLds {
-    static constexpr int PHASES = 4 / RG;                                            // tiles of 32 tokens at a time
-    static constexpr int STAGE = 32 * PHASES > 4096 / D ? 32 * PHASES : 4096 / D;    // tokens: a 128-bit load of K or V a thread, or two
+    static constexpr int STAGE = 64;
     static constexpr int PITCHK = 2 * D + 16, PITCHV = 2 * D + 64;
     static constexpr int STAGE_BYTES = STAGE * (PITCHK + PITCHV) + 8 * STAGE;
     static constexpr int BYTES = 2 * STAGE_BYTES;
 };
 
-// RG groups of 32 rows (2 or 4), q_row(i) row i's queries, record(i, phase) the index of its record; tokens [t_begin, t_end) of the T
+// RG groups of 32 rows: 4, a wave has a stage's two tiles, or 2, and a wave has one of them (phase 0 or 1).  q_row(i): row i's queries,
+// record(i, phase): the index of its record; tokens [t_begin, t_end) of the T.
+// What a tile costs a wave: 16 matrix instructions (512 cycles of D = 128) and some 190 vector ones, 16 exponentials among them (the codes'
+// conversions for the workgroup, a fourth each, 60).  In the order of the formulas the one waits for the other and both for LDS, and two
+// waves a SIMD do not fill that (1500 cycles a tile); so the steps of both products carry, one for one, a piece of something else: the
+// first's the conversion of the next stage, the second's the exponentials of the tokens behind.
 template <int D, int RG, class QRow, class Record>
 __device__ __forceinline__ void prefix_sweep(char* const smem, const QRow q_row, const int n_rows, const int8_t* kc, const float* ks,
                                              const int8_t* vc, const float* vs, const int T, const int t_begin, const int t_end,
                                              const float scale_log2e, const Record record, float* ws_acc, float* ws_ml) {
-    using Lds = PrefixLds<D, RG>;
+    using Lds = PrefixLds<D>;
     constexpr int KS = D / 16, DT = D / 32;            // k-steps of the score MFMA, 32-row tiles of O^T
-    constexpr int STAGE = Lds::STAGE, PHASES = Lds::PHASES, PITCHK = Lds::PITCHK, PITCHV = Lds::PITCHV;
+    constexpr int STAGE = Lds::STAGE, PITCHK = Lds::PITCHK, PITCHV = Lds::PITCHV;
+    constexpr int NT = RG / 2;                         // tiles a wave and stage
     constexpr int NP = STAGE * D / 4096;               // 128-bit loads a thread, stage and tensor
-    constexpr int SUB = STAGE / (32 * PHASES);         // tiles a wave and stage
+    static_assert(4 * NP == KS, "a piece of the next stage for each k-step");
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l32 = lane & 31, hh = lane >> 5;
     const int rg = w % RG, phase = w / RG;
-    const bool busy = 32 * rg < n_rows;                // (uniform)
 
     // Q^T B operands: lane holds row l32, d = 16 s + 8 hh + [0,8)
     bf16x8 qB[KS];
@@ -59,129 +63,180 @@ __device__ __forceinline__ void prefix_sweep(char* const smem, const QRow q_row,
     }
     const __amdgpu_buffer_rsrc_t krs = __builtin_amdgcn_make_buffer_rsrc((void*)kc, 0, (int)((unsigned)T * D), 0x00020000);
     const __amdgpu_buffer_rsrc_t vrs = __builtin_amdgcn_make_buffer_rsrc((void*)vc, 0, (int)((unsigned)T * D), 0x00020000);
-    const __amdgpu_buffer_rsrc_t ksr = __builtin_amdgcn_make_buffer_rsrc((void*)ks, 0, (int)((unsigned)T * 4u), 0x00020000);
-    const __amdgpu_buffer_rsrc_t vsr = __builtin_amdgcn_make_buffer_rsrc((void*)vs, 0, (int)((unsigned)T * 4u), 0x00020000);
-    u32x4 kbuf[NP], vbuf[NP];
-    uint32_t sc = 0u;
-    // (rows past the end of the prefix read as zeros and are masked; threads without a scale ask past the end)
-    const int off_ks = tid < STAGE ? tid * 4 : (int)0x7ffffff0, off_vs = tid >= 64 && tid < 64 + STAGE ? (tid - 64) * 4 : (int)0x7ffffff0;
-    auto issue = [&](int t0) {
+    // (rows past the end of the prefix read as zeros and are masked.  Wave 0 has the stage's K scales, wave 1 its V scales, the
+    // others ask past the end: a load is the same instructions for all)
+    const __amdgpu_buffer_rsrc_t srs = __builtin_amdgcn_make_buffer_rsrc((void*)(w == 1 ? vs : ks), 0, w < 2 ? (int)((unsigned)T * 4u) : 0, 0x00020000);
+    u32x4 buf[2][2][NP];                               // two stages in flight
+    uint32_t sc[2];
+    auto issue = [&](auto set_c, int t0) __attribute__((always_inline)) {
+        constexpr int set = decltype(set_c)::value;
         const int base = t0 < t_end ? t0 : T;          // (a stage that is not wanted: nothing is read)
+        const int off = (int)((unsigned)base * D + (unsigned)(tid * 16));
 #pragma unroll
-        for (int n = 0; n < NP; ++n) {
-            kbuf[n] = __builtin_amdgcn_raw_buffer_load_b128(krs, (int)((unsigned)base * D + (unsigned)(tid * 16 + n * 4096)), 0, 0);
-            vbuf[n] = __builtin_amdgcn_raw_buffer_load_b128(vrs, (int)((unsigned)base * D + (unsigned)(tid * 16 + n * 4096)), 0, 0);
-        }
-        sc = __builtin_amdgcn_raw_buffer_load_b32(ksr, off_ks + base * 4, 0, 0) | __builtin_amdgcn_raw_buffer_load_b32(vsr, off_vs + base * 4, 0, 0);
-    };
-    auto widen16 = [&](const u32x4 c, char* to) {      // 16 codes -> 16 bf16, exact
-        *reinterpret_cast<bf16x8*>(to) = widen8(i32x2{(int)c[0], (int)c[1]});
-        *reinterpret_cast<bf16x8*>(to + 16) = widen8(i32x2{(int)c[2], (int)c[3]});
-    };
-    auto stage = [&](char* buf) {
-        char* const vS = buf + STAGE * PITCHK;
+        for (int n = 0; n < NP; ++n) buf[set][0][n] = __builtin_amdgcn_raw_buffer_load_b128(krs, off + n * 4096, 0, 0);
 #pragma unroll
-        for (int n = 0; n < NP; ++n) {
-            const int at = tid * 16 + n * 4096, row = at / D, col = at % D;
-            widen16(kbuf[n], buf + row * PITCHK + col * 2);
-            widen16(vbuf[n], vS + row * PITCHV + col * 2);
-        }
-        float* const scS = reinterpret_cast<float*>(vS + STAGE * PITCHV);   // [0, STAGE) k_scale * c, then v_scale
-        const float s = __uint_as_float(sc);
-        if (tid < STAGE) scS[tid] = s * scale_log2e;
-        else if (tid >= 64 && tid < 64 + STAGE) scS[STAGE + tid - 64] = s;
+        for (int n = 0; n < NP; ++n) buf[set][1][n] = __builtin_amdgcn_raw_buffer_load_b128(vrs, off + n * 4096, 0, 0);
+        sc[set] = __builtin_amdgcn_raw_buffer_load_b32(srs, (base + lane) * 4, 0, 0);
     };
-    static_assert(STAGE <= 64, "a wave has the K scales, the next one the V scales");
+    // piece i of a stage on its way into LDS: 8 codes of K (the first half) or V -> 8 bf16, exact
+    auto piece = [&](int set, char* to, int i) __attribute__((always_inline)) {
+        const int x = i / (2 * NP), n = i / 2 % NP, half = i % 2;
+        const int at = tid * 16 + n * 4096, row = at / D, col = at % D;
+        char* const dst = to + (x == 0 ? row * PITCHK : STAGE * PITCHK + row * PITCHV) + col * 2 + 16 * half;
+        *reinterpret_cast<bf16x8*>(dst) = widen8(i32x2{(int)buf[set][x][n][2 * half], (int)buf[set][x][n][2 * half + 1]});
+    };
+    auto scales = [&](int set, char* to) __attribute__((always_inline)) {   // [0, STAGE) k_scale * c, then v_scale
+        float* const scS = reinterpret_cast<float*>(to + STAGE * (PITCHK + PITCHV));
+        const float s = __uint_as_float(sc[set]);
+        if (w < 2) scS[64 * w + lane] = w == 0 ? s * scale_log2e : s;
+    };
 
-    const int k_addr = l32 * PITCHK + 16 * hh;   // K fragment of k-step s: row l32, bytes 32 s + 16 hh + [0,16)
+    const int tile0 = NT == 1 ? 32 * phase : 0;  // of the stage
+    const int k_addr = (tile0 + l32) * PITCHK + 16 * hh;   // K fragment of k-step s: row l32, bytes 32 s + 16 hh + [0,16)
     // V transpose reads: 16 lanes fetch rows k..k+3, lane i receives column i of them
-    const int v_addr = (4 * hh + ((lane & 15) >> 2)) * PITCHV + (2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) * 16 + 8 * (lane & 1);
+    const int v_addr = STAGE * PITCHK + (tile0 + 4 * hh + ((lane & 15) >> 2)) * PITCHV + (2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) * 16 + 8 * (lane & 1);
     f32x16 o[DT];
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[dt][r] = 0.0f;
-    float M = kMasked, lsum = 0.0f;   // running max of this lane's row (log2 units), this lane's part of the row sum
+    float M = 0.0f, lsum = 0.0f;   // running max of this lane's row (log2 units), this lane's part of the row sum
+    bool first = true;             // (uniform)
 
-    issue(t_begin);
-    stage(smem);
-    issue(t_begin + STAGE);
+    const std::integral_constant<int, 0> set0{};
+    const std::integral_constant<int, 1> set1{};
+    issue(set0, t_begin);
+    issue(set1, t_begin + STAGE);
+#pragma unroll
+    for (int i = 0; i < KS; ++i) piece(0, smem, i);
+    scales(0, smem);
+    issue(set0, t_begin + 2 * STAGE);
     __syncthreads();
-    int turn = 0;
-    for (int t0 = t_begin; t0 < t_end; t0 += STAGE, turn ^= 1) {
+    // the stage from token t0 on, in LDS buffer `turn`; the one behind it goes into the other, which every wave is done with since the
+    // last barrier
+    auto work = [&](auto turn_c, int t0) __attribute__((always_inline)) {
+        constexpr int turn = decltype(turn_c)::value;
         const char* const kS = smem + turn * Lds::STAGE_BYTES;
-        const char* const vS = kS + STAGE * PITCHK;
-        const float* const scS = reinterpret_cast<const float*>(vS + STAGE * PITCHV);
-        stage(smem + (turn ^ 1) * Lds::STAGE_BYTES);   // (the other stage: every wave is done with it since the last barrier)
-        issue(t0 + 2 * STAGE);
+        char* const next = smem + (turn ^ 1) * Lds::STAGE_BYTES;
+        const float* const scS = reinterpret_cast<const float*>(kS + STAGE * (PITCHK + PITCHV)) + tile0 + 4 * hh;
+        scales(turn ^ 1, next);
+        f32x16 u[NT];
 #pragma unroll
-        for (int x = 0; x < SUB; ++x) {
-            const int tile = (phase + x * PHASES) * 32, tt = t0 + tile;
-            if (!busy || tt >= t_end) continue;        // (uniform)
-            const char* const kT = kS + tile * PITCHK;
-            const char* const vT = vS + tile * PITCHV;
-            f32x16 acc;
+        for (int t = 0; t < NT; ++t)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) acc[r] = 0.0f;
+            for (int r = 0; r < 16; ++r) u[t][r] = 0.0f;
+        bf16x8 kf[2][NT];
 #pragma unroll
-            for (int s = 0; s < KS; ++s)
-                acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(kT + k_addr + 32 * s), qB[s], acc, 0, 0, 0);
-            // register r of this lane is token tt + 8 (r/4) + 4 hh + r%4
-            float u[16];
+        for (int t = 0; t < NT; ++t) kf[0][t] = *reinterpret_cast<const bf16x8*>(kS + k_addr + t * 32 * PITCHK);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int r4 = 0; r4 < 4; ++r4) {
-                const f32x4 f = *reinterpret_cast<const f32x4*>(&scS[tile + 8 * r4 + 4 * hh]);
+        for (int s = 0; s < KS; ++s) {
+            if (s + 1 < KS) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) u[4 * r4 + e] = acc[4 * r4 + e] * f[e];
+                for (int t = 0; t < NT; ++t) kf[(s + 1) & 1][t] = *reinterpret_cast<const bf16x8*>(kS + k_addr + t * 32 * PITCHK + 32 * (s + 1));
             }
-            if (tt + 32 > T) {
 #pragma unroll
-                for (int r = 0; r < 16; ++r) u[r] = tt + 8 * (r / 4) + 4 * hh + r % 4 < T ? u[r] : kMasked;
-            }
-            float umax = fmaxf(u[0], u[1]);
-#pragma unroll
-            for (int r = 2; r < 16; r += 2) umax = fmaxf(umax, fmaxf(u[r], u[r + 1]));
-            // the running max, a whole number (decode_gqa.hip says why), moves only when a score has passed it by 2^8
-            if (__builtin_amdgcn_ballot_w64(umax - M > 8.0f) != 0) {
-                const float m_new = ceilf(fmaxf(M, half_max(umax)));
-                const float alpha = fast_exp2(M - m_new);
-#pragma unroll
-                for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) o[dt][r] *= alpha;
-                lsum *= alpha;
-                M = m_new;
-            }
-            float ps0 = 0.0f, ps1 = 0.0f;
-#pragma unroll
-            for (int r = 0; r < 16; r += 2) {
-                u[r] = fast_exp2(u[r] - M);
-                u[r + 1] = fast_exp2(u[r + 1] - M);
-                ps0 += u[r];
-                ps1 += u[r + 1];
-            }
-            lsum += ps0 + ps1;
-            // the probabilities take their token's v_scale before they are rounded to bf16, operands of the second product
-            u32x4 pw[2];
-#pragma unroll
-            for (int r4 = 0; r4 < 4; ++r4) {
-                const f32x4 f = *reinterpret_cast<const f32x4*>(&scS[STAGE + tile + 8 * r4 + 4 * hh]);
-                pw[r4 >> 1][2 * (r4 & 1)] = pack_bf16x2(u[4 * r4] * f[0], u[4 * r4 + 1] * f[1]);
-                pw[r4 >> 1][2 * (r4 & 1) + 1] = pack_bf16x2(u[4 * r4 + 2] * f[2], u[4 * r4 + 3] * f[3]);
-            }
-            // O^T += V^T P^T: k-step u2 covers tokens 16 u2 + {4 hh .. 4 hh + 3} and 16 u2 + 8 + {4 hh .. 4 hh + 3} of the tile
-#pragma unroll
-            for (int u2 = 0; u2 < 2; ++u2)
-#pragma unroll
-                for (int dt = 0; dt < DT; ++dt) {
-                    const char* va = vT + v_addr + 64 * dt + 16 * u2 * PITCHV;
-                    const s16x4 lo = lds_read_tr16(reinterpret_cast<const uint16_t*>(va));
-                    const s16x4 hi = lds_read_tr16(reinterpret_cast<const uint16_t*>(va + 8 * PITCHV));
-                    const s16x8 av = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-                    o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, av), __builtin_bit_cast(bf16x8, pw[u2]), o[dt], 0, 0, 0);
-                }
+            for (int t = 0; t < NT; ++t) u[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[s & 1][t], qB[s], u[t], 0, 0, 0);
+            piece(turn ^ 1, next, s);
+            __builtin_amdgcn_sched_barrier(0);
         }
+        f32x4 kscale[NT][4];
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int r4 = 0; r4 < 4; ++r4) kscale[t][r4] = *reinterpret_cast<const f32x4*>(scS + 32 * t + 8 * r4);
+        // V fragments of k-step x of the second product (tokens 16 x + ...): two ahead of their use
+        s16x4 vf[2][DT][2];
+        auto fetch_v = [&](int x) __attribute__((always_inline)) {
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) {
+                const char* va = kS + v_addr + 64 * dt + 16 * x * PITCHV;
+                vf[x & 1][dt][0] = lds_read_tr16(reinterpret_cast<const uint16_t*>(va));
+                vf[x & 1][dt][1] = lds_read_tr16(reinterpret_cast<const uint16_t*>(va + 8 * PITCHV));
+            }
+        };
+        f32x4 vscale[2][2];
+        auto fetch_scales = [&](int x) __attribute__((always_inline)) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) vscale[x & 1][i] = *reinterpret_cast<const f32x4*>(scS + STAGE + 16 * x + 8 * i);
+        };
+        fetch_scales(0);
+        fetch_scales(1);
+        fetch_v(0);
+        __builtin_amdgcn_sched_barrier(0);
+        // register r of u[t] is token t0 + tile0 + 32 t + 8 (r/4) + 4 hh + r%4; scores relative to the running max
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) u[t][r] = fmaf(u[t][r], kscale[t][r / 4][r % 4], -M);
+        __builtin_amdgcn_sched_barrier(0);
+        issue(std::integral_constant<int, turn ^ 1>{}, t0 + 3 * STAGE);   // (here, where registers are free again)
+        if (t0 + STAGE > T) {
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) u[t][r] = t0 + tile0 + 32 * t + 8 * (r / 4) + 4 * hh + r % 4 < T ? u[t][r] : kMasked;
+        }
+        float umax = u[0][0];
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int r = 0; r < 16; r += 2) umax = fmaxf(umax, fmaxf(u[t][r], u[t][r + 1]));
+        // the running max, a whole number (decode_gqa.hip says why), moves only when a score has passed it by 2^8, but for the first
+        // stage, which sets it
+        if (first || __builtin_amdgcn_ballot_w64(umax > 8.0f) != 0) {
+            // (a tile past the end, of a wave that has no other: nothing, but finite)
+            const float up = fmaxf(ceilf(half_max(umax)), 0.1f * kMasked), by = first ? up : fmaxf(up, 0.0f);
+            const float alpha = first ? 0.0f : fast_exp2(-by);   // (nothing to rescale yet)
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) o[dt][r] *= alpha;
+            lsum *= alpha;
+            M += by;
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) u[t][r] -= by;
+            first = false;
+        }
+        // O^T += V^T P^T: k-step x covers tokens 16 x + {4 hh .. 4 hh + 3} and 16 x + 8 + {4 hh .. 4 hh + 3}, registers 8 x to 8 x + 7; the
+        // probabilities take their token's v_scale before they are rounded to bf16, operands of the product
+        u32x4 pw[2];
+        float ps = 0.0f;
+        auto probabilities = [&](int x, int e) __attribute__((always_inline)) {   // registers 8 x + 2 e and the next
+            const int t = x / 2, r = 8 * (x % 2) + 2 * e;
+            const f32x4 f = vscale[x & 1][e / 2];
+            const float a = fast_exp2(u[t][r]), b = fast_exp2(u[t][r + 1]);
+            ps += a + b;
+            pw[x & 1][e] = pack_bf16x2(a * f[2 * (e % 2)], b * f[2 * (e % 2) + 1]);
+        };
+#pragma unroll
+        for (int e = 0; e < 4; ++e) probabilities(0, e);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int x = 0; x < 2 * NT; ++x) {
+            if (x + 1 < 2 * NT) fetch_v(x + 1);
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) {
+                const s16x4 lo = vf[x & 1][dt][0], hi = vf[x & 1][dt][1];
+                const s16x8 av = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+                o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, av), __builtin_bit_cast(bf16x8, pw[x & 1]), o[dt], 0, 0, 0);
+                if (x + 1 < 2 * NT)
+#pragma unroll
+                    for (int e = 0; e < 4 / DT; ++e) probabilities(x + 1, dt * (4 / DT) + e);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            if (x + 2 < 2 * NT) fetch_scales(x + 2);
+        }
+        lsum += ps;
         __syncthreads();
+    };
+    for (int t0 = t_begin;; t0 += 2 * STAGE) {   // (at least one stage)
+        work(set0, t0);
+        if (t0 + STAGE >= t_end) break;
+        work(set1, t0 + STAGE);
+        if (t0 + 2 * STAGE >= t_end) break;
     }
     const float L = half_sum(lsum);
     const int row = 32 * rg + l32;
@@ -215,10 +270,10 @@ struct PrefixParams {
 // FORM: rows of the prefix's workgroups: 1, 2: 16 or 32, waves of their own; 3, 4: 64 or 128, shared tiles.  NC: groups of 16 query
 // heads of the own caches' workgroups.
 template <int D, int FORM, int NC>
-__global__ __launch_bounds__(256) void slim_decode_prefix_kernel(const PrefixParams p) {
+__global__ __launch_bounds__(256, 2) void slim_decode_prefix_kernel(const PrefixParams p) {
     constexpr int RG = FORM == 4 ? 4 : 2;
     constexpr int OWN_LDS = 4 * GqaLds<D, NC>::WAVE_BYTES;
-    constexpr int SHARED_LDS = FORM >= 3 ? PrefixLds<D, RG>::BYTES : 4 * GqaLds<D, (FORM < 3 ? FORM : 1)>::WAVE_BYTES;
+    constexpr int SHARED_LDS = FORM >= 3 ? PrefixLds<D>::BYTES : 4 * GqaLds<D, (FORM < 3 ? FORM : 1)>::WAVE_BYTES;
     __shared__ __attribute__((aligned(16))) char smem[OWN_LDS > SHARED_LDS ? OWN_LDS : SHARED_LDS];
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int Hq = p.G * p.Hkv;
@@ -234,7 +289,7 @@ __global__ __launch_bounds__(256) void slim_decode_prefix_kernel(const PrefixPar
             return (long)b * Hq + g * p.G + (r - b * p.G);
         };
         if constexpr (FORM >= 3) {
-            constexpr int STAGE = PrefixLds<D, RG>::STAGE, PHASES = PrefixLds<D, RG>::PHASES;
+            constexpr int STAGE = PrefixLds<D>::STAGE, PHASES = 4 / RG;
             int first, end;
             split_span((p.P + STAGE - 1) / STAGE, p.n_prefix / PHASES, sp, first, end);
             prefix_sweep<D, RG>(smem, [&](int i) { return p.q + row_of(i) * D; }, n_rows, p.pkc + kv0 * D, p.pks + kv0, p.pvc + kv0 * D,
@@ -308,17 +363,19 @@ static PrefixPlan prefix_plan(int batch, int q_heads, int kv_heads, int prefix_l
     plan.form = rows <= 16 ? 1 : rows <= 32 ? 2 : rows <= 64 ? 3 : 4;
     plan.row_blocks = (int)((rows + 127) / 128);
     plan.head_groups = (G + 31) / 32;
+    // The prefix: a workgroup a compute unit, beside which there is room for one of an own cache, or two where each still has 32 stages
+    // (64 on 8 heads, 64 sequences, P=32768 104.6 and 93.1 us); and none with less than 8 stages, as every one
+    // costs a record of its rows besides (the same heads, 128 sequences, P=1000, T=300 32.3 us with 4, 28.9 with 8).  Up to 32 rows a record
+    // is little: two tiles a wave (32 on 8 heads, 2 sequences, P=4000, T=100 14.0 us with 8, 11.0 with 4, 9.5).
     const int phases = plan.form == 3 ? 2 : 1;
-    const long items = (long)kv_heads * plan.row_blocks, stage = plan.form < 3 ? 128 : plan.form == 3 ? 64 : 4096 / head_dim;
-    const long most = (prefix_len + stage * 4 - 1) / (stage * 4);
-    long n = (512 + items - 1) / items;
-    n = n < most ? n : most;
-    plan.n_prefix = (int)(n < 1 ? 1 : n) * phases;
+    const long items = (long)kv_heads * plan.row_blocks, stages = ((long)prefix_len + (plan.form < 3 ? 127 : 63)) / (plan.form < 3 ? 128 : 64);
+    long n = (256 + items - 1) / items;
+    if (plan.form >= 3 && stages / (2 * n) >= 32) n *= 2;
+    const long least = plan.form < 3 ? 2 : 8;
+    n = std::min(n, (stages + least - 1) / least);
+    plan.n_prefix = (int)n * phases;
     const long own = (long)batch * kv_heads * plan.head_groups;
-    n = (512 + own - 1) / own;
-    const long most_own = ((long)kv_len + 255) / 256;
-    n = n < most_own ? n : most_own;
-    plan.n_own = (int)(n < 1 ? 1 : n);
+    plan.n_own = (int)std::min((512 + own - 1) / own, ((long)kv_len + 255) / 256);
     return plan;
 }
 

@@ -98,7 +98,7 @@ __global__ __launch_bounds__(256) void slim_qk_norm_rope_kernel(const RopeArgs p
         const int pos = p.positions[token];
         const bool there = pos >= 0 && pos < p.table_len;
         const long slot = APPEND ? (long)p.slots[b] + s : s;
-        const bool room = there && slot >= 0 && slot < p.kv_len;
+        const bool room = slot >= 0 && slot < p.kv_len;
         double cs[4], sn[4];
         {
             const float* t = p.cos_sin + (long)(there ? pos : 0) * D + 4 * c;
@@ -109,14 +109,35 @@ __global__ __launch_bounds__(256) void slim_qk_norm_rope_kernel(const RopeArgs p
                 sn[i] = (double)ts[i];
             }
         }
+        // unit u's kind (uniform), and this lane's head of it: past the last one that head's again, which is not stored
+        auto unit = [&](int u, int& kind, int& heads, int& h) {
+            kind = u < uq ? 0 : u < uq + uk ? 1 : 2;
+            heads = kind == 0 ? p.q_heads : p.kv_heads;
+            h = (u - (kind == 0 ? 0 : kind == 1 ? uq : uq + uk)) * RW + sub;
+        };
+        auto load = [&](int u) {
+            int kind, heads, h;
+            unit(u, kind, heads, h);
+            return load_piece<D, PAIRS>((const uint16_t*)(kind == 0 ? p.q : kind == 1 ? p.k : p.v) +
+                                            token * (kind == 0 ? p.q_stride : kind == 1 ? p.k_stride : p.v_stride) + (long)min(h, heads - 1) * D, c);
+        };
+        u32x4 raw_next = load(part * per_part);
+        if (!there) {   // (uniform) padding: rows of zeros, nothing into the cache, no more of its rows read
+            for (int u = part * per_part; u < (APPEND ? min(u_end, uq) : u_end); ++u) {
+                int kind, heads, h;
+                unit(u, kind, heads, h);
+                uint16_t* dst = (uint16_t*)(kind == 0 ? p.q_out : kind == 1 ? p.k_out : p.v_out) +
+                                (((long)b * heads + min(h, heads - 1)) * p.seq_len + s) * D;
+                if (h < heads) store_piece<D, PAIRS>(dst, c, u32x4{0u, 0u, 0u, 0u});
+            }
+            continue;
+        }
         for (int u = part * per_part; u < u_end; ++u) {
-            const int kind = u < uq ? 0 : u < uq + uk ? 1 : 2;   // (uniform)
-            const int heads = kind == 0 ? p.q_heads : p.kv_heads;
-            const int h = (u - (kind == 0 ? 0 : kind == 1 ? uq : uq + uk)) * RW + sub;
-            const int hc = min(h, heads - 1);   // (a row past the last head: that head's again, not stored)
-            const uint16_t* src = (const uint16_t*)(kind == 0 ? p.q : kind == 1 ? p.k : p.v) +
-                                  token * (kind == 0 ? p.q_stride : kind == 1 ? p.k_stride : p.v_stride) + (long)hc * D;
-            u32x4 raw = load_piece<D, PAIRS>(src, c);
+            int kind, heads, h;
+            unit(u, kind, heads, h);
+            const int hc = min(h, heads - 1);
+            u32x4 raw = raw_next;
+            raw_next = load(min(u + 1, u_end - 1));
             if (kind < 2) {
                 const uint16_t* wt = (const uint16_t*)(kind == 0 ? p.q_weight : p.k_weight);
                 double x[8];
@@ -145,7 +166,7 @@ __global__ __launch_bounds__(256) void slim_qk_norm_rope_kernel(const RopeArgs p
             if (!APPEND || kind == 0) {
                 uint16_t* dst = (uint16_t*)(kind == 0 ? p.q_out : kind == 1 ? p.k_out : p.v_out) +
                                 (((long)b * heads + hc) * p.seq_len + s) * D;
-                if (h < heads) store_piece<D, PAIRS>(dst, c, there ? raw : u32x4{0u, 0u, 0u, 0u});
+                if (h < heads) store_piece<D, PAIRS>(dst, c, raw);
             } else {
                 u32x2 codes;
                 float scale;
@@ -169,11 +190,13 @@ __global__ __launch_bounds__(256) void slim_qk_norm_rope_kernel(const RopeArgs p
 hipError_t launch_qk_norm_rope(const RopeArgs& a, bool append, hipStream_t stream) {
     const int rw = 512 / a.head_dim, units = (a.q_heads + rw - 1) / rw + 2 * ((a.kv_heads + rw - 1) / rw);
     const long tokens = (long)a.batch * a.seq_len;
-    // a wave for each unit of heads where tokens are few, several units a wave (its position, angles and weights once) where
-    // that still leaves 8192 waves
+    // a wave for each unit of heads where tokens are few, up to six units a wave (its position, angles and weights once) where
+    // that leaves 8192 waves: 32 heads, 2048 tokens 29.9 us with one unit a wave, 25.2 with two, 23.6 with six, 28.7 with twelve; 8192
+    // tokens, 64 on 8 heads 94.4, 75.0, 72.1, 72.3
     long per = tokens * units / 8192;
-    per = per < 1 ? 1 : per > units ? units : per;
+    per = per < 1 ? 1 : per > 6 ? 6 : per;
     const int parts = (units + (int)per - 1) / (int)per;
+    per = (units + parts - 1) / parts;
     // (the loop over items is for more tokens than this many workgroups)
     const dim3 grid((unsigned)std::min((tokens * parts + 3) / 4, 1L << 22)), block(256);
     auto launch = [&](auto d_c, auto pairs_c, auto append_c) {

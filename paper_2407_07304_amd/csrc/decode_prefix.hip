@@ -364,14 +364,15 @@ static PrefixPlan prefix_plan(int batch, int q_heads, int kv_heads, int prefix_l
     plan.row_blocks = (int)((rows + 127) / 128);
     plan.head_groups = (G + 31) / 32;
     // The prefix: a workgroup a compute unit, beside which there is room for one of an own cache, or two where each still has 32 stages
-    // (64 on 8 heads, 64 sequences, P=32768 104.6 and 93.1 us); and none with less than 8 stages, as every one
-    // costs a record of its rows besides (the same heads, 128 sequences, P=1000, T=300 32.3 us with 4, 28.9 with 8).  Up to 32 rows a record
-    // is little: two tiles a wave (32 on 8 heads, 2 sequences, P=4000, T=100 14.0 us with 8, 11.0 with 4, 9.5).
+    // (64 on 8 heads, 64 sequences, P=32768 104.6 and 93.1 us); and none with less than 4 stages, 8 from 2048
+    // query rows on, as every one costs a record of its rows besides (32 on 8 heads, 48 sequences, P=1024, T=100 with 1, 4 and 8 stages 21.3,
+    // 14.8 and 19.6 us; 64 on 8 heads, 128 sequences, P=512 27.0, 22.8 and 23.7; 32 heads, 128 sequences, P=2000 44.6, 44.6 and 38.9).  Up to 32
+    // rows a record is little: two tiles a wave (32 on 8 heads, 2 sequences, P=4000, T=100 14.0 us with 8, 11.0 with 4, 9.5).
     const int phases = plan.form == 3 ? 2 : 1;
     const long items = (long)kv_heads * plan.row_blocks, stages = ((long)prefix_len + (plan.form < 3 ? 127 : 63)) / (plan.form < 3 ? 128 : 64);
     long n = (256 + items - 1) / items;
     if (plan.form >= 3 && stages / (2 * n) >= 32) n *= 2;
-    const long least = plan.form < 3 ? 2 : 8;
+    const long least = plan.form < 3 ? 2 : (long)batch * q_heads < 2048 ? 4 : 8;
     n = std::min(n, (stages + least - 1) / least);
     plan.n_prefix = (int)n * phases;
     const long own = (long)batch * kv_heads * plan.head_groups;

@@ -175,7 +175,7 @@ __device__ __forceinline__ void prefix_sweep(char* const smem, const QRow q_row,
 #pragma unroll
             for (int t = 0; t < NT; ++t)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) u[t][r] = t0 + tile0 + 32 * t + 8 * (r / 4) + 4 * hh + r % 4 < T ? u[t][r] : kMasked;
+                for (int r = 0; r < 16; ++r) u[t][r] = t0 + tile0 + 32 * t + 8 * (r / 4) + 4 * hh + r % 4 < T ? u[t][r] : -INFINITY;
         }
         float umax = u[0][0];
 #pragma unroll
@@ -183,10 +183,9 @@ __device__ __forceinline__ void prefix_sweep(char* const smem, const QRow q_row,
 #pragma unroll
             for (int r = 0; r < 16; r += 2) umax = fmaxf(umax, fmaxf(u[t][r], u[t][r + 1]));
         // the running max, a whole number (decode_gqa.hip says why), moves only when a score has passed it by 2^8, but for the first
-        // stage, which sets it
-        if (first || __builtin_amdgcn_ballot_w64(umax > 8.0f) != 0) {
-            // (a tile past the end, of a wave that has no other: nothing, but finite)
-            const float up = fmaxf(ceilf(half_max(umax)), 0.1f * kMasked), by = first ? up : fmaxf(up, 0.0f);
+        // stage, which sets it (not if the wave's tile of it is past the end: it has no other)
+        if (t0 + tile0 < T && (first || __builtin_amdgcn_ballot_w64(umax > 8.0f) != 0)) {
+            const float up = ceilf(half_max(umax)), by = first ? up : fmaxf(up, 0.0f);
             const float alpha = first ? 0.0f : fast_exp2(-by);   // (nothing to rescale yet)
 #pragma unroll
             for (int dt = 0; dt < DT; ++dt)
@@ -248,7 +247,7 @@ __device__ __forceinline__ void prefix_sweep(char* const smem, const QRow q_row,
             for (int r4 = 0; r4 < 4; ++r4)
                 *reinterpret_cast<f32x4*>(ws_acc + idx * D + 32 * dt + 8 * r4 + 4 * hh) =
                     f32x4{o[dt][4 * r4], o[dt][4 * r4 + 1], o[dt][4 * r4 + 2], o[dt][4 * r4 + 3]};
-        if (hh == 0) reinterpret_cast<f32x2*>(ws_ml)[idx] = f32x2{M, L};
+        if (hh == 0) reinterpret_cast<f32x2*>(ws_ml)[idx] = f32x2{first ? kNone : M, L};   // (nothing: behind everything)
     }
 }
 

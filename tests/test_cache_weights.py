@@ -136,6 +136,30 @@ def test_weights_of_sharp_rows_and_zero_tokens(sa, B, Hq, Hkv, T):
 
 
 @gpu
+@pytest.mark.parametrize("B,Hq,Hkv,T", [(2, 8, 2, 1500), (60, 8, 4, 200)])
+def test_weights_of_extreme_queries(sa, B, Hq, Hkv, T):
+    """Rows around 2^-50: every token the same weight.  Rows around 2^60: the largest score has all of it.  A row that is not finite shows
+    in its own result and its KV head's weights alone."""
+    rng = np.random.default_rng(T)
+    D, scale = 64, 0.125
+    own = [*cache(rng, B, Hkv, T, D), *cache(rng, B, Hkv, T, D)]
+    lens = torch.from_numpy(rng.integers(1, T + 1, B).astype(np.int32))
+    q = torch.from_numpy(rng.standard_normal((B, Hq, 1, D), dtype=np.float32)).to(BF16)
+    check(sa, (q.float() * 2.0 ** -50).to(BF16), own, lens, scale, "2^-50")
+    big = (q.float() * 2.0 ** 60).to(BF16)
+    want, o_bound, w, _ = reference(big, own, lens, scale)
+    out, got = sa.slim_attn_decode_int8_weights(big.cuda(), *on_gpu(own), lens.cuda(), scale)
+    assert ((out.double().cpu() - want).abs() <= o_bound).all() and torch.equal(got.double().cpu(), w.round())
+    out, fine = sa.slim_attn_decode_int8_weights(q.cuda(), *on_gpu(own), lens.cuda(), scale)
+    q[1, 1, 0, 3] = math.nan
+    bad, got = sa.slim_attn_decode_int8_weights(q.cuda(), *on_gpu(own), lens.cuda(), scale)
+    assert torch.equal((bad != out).any(-1).nonzero().cpu(), torch.tensor([[1, 1, 0]]))
+    same = (got == fine).all(-1)
+    same[1, 1 // (Hq // Hkv)] = True
+    assert same.all()
+
+
+@gpu
 def test_weights_in_place_over_steps_streams_and_replays(sa):
     """weights_out == weights_in adds up; lengths out of range are the nearest bound; two streams and a graph give the same bits."""
     rng = np.random.default_rng(2)

@@ -162,6 +162,46 @@ def test_shared_prefix_all_zero_tokens_and_huge_scores(sa, B, Hq, Hkv):
 
 
 @gpu
+@pytest.mark.parametrize("B,Hq,Hkv", [(2, 8, 2), (6, 8, 2), (12, 8, 2), (40, 8, 2)])
+@pytest.mark.parametrize("D", [64, 128])
+def test_shared_prefix_of_extreme_queries(sa, B, Hq, Hkv, D):
+    """Rows around 2^60 (the largest score alone counts) and 2^-50 (every token the same), the prefix ending inside a tile; and a row
+    that is not finite, which no other row shows."""
+    rng = np.random.default_rng(D + B)
+    P, T, scale = 777, 90, 1 / math.sqrt(D)
+    prefix, own = [*cache(rng, 1, Hkv, P, D), *cache(rng, 1, Hkv, P, D)], [*cache(rng, B, Hkv, T, D), *cache(rng, B, Hkv, T, D)]
+    lens = torch.from_numpy(rng.integers(0, T + 1, B).astype(np.int32))
+    q = queries(rng, B, Hq, D)
+    for shift in (60, -50):
+        qs = (q.float() * 2.0 ** shift).to(BF16)
+        want, bound = reference(qs, prefix, own, lens, scale)
+        got = sa.slim_attn_decode_int8_shared_prefix(qs.cuda(), *on_gpu(prefix), *on_gpu(past_the_end(own, lens)), lens.cuda(), scale)
+        assert ((got.double().cpu() - want).abs() <= bound).all(), shift
+    fine = sa.slim_attn_decode_int8_shared_prefix(q.cuda(), *on_gpu(prefix), *on_gpu(own), lens.cuda(), scale)
+    for bad in (math.inf, -math.inf, math.nan):
+        qn = q.clone()
+        qn[1, 3, 0, 5] = bad
+        got = sa.slim_attn_decode_int8_shared_prefix(qn.cuda(), *on_gpu(prefix), *on_gpu(own), lens.cuda(), scale)
+        off = (got != fine).any(-1)
+        assert torch.equal(off.nonzero().cpu(), torch.tensor([[1, 3, 0]])) and not torch.isfinite(got[1, 3]).any()
+
+
+@gpu
+@pytest.mark.parametrize("B", [2, 6, 12, 40])
+def test_shared_prefix_of_very_low_scores(sa, B):
+    """All scores of a row around -2^100, where they are all the same in fp32: the mean of the values, without what lies past the end."""
+    rng = np.random.default_rng(7)
+    Hq, Hkv, D, P, T = 8, 2, 128, 333, 1
+    prefix, own = [*cache(rng, 1, Hkv, P, D), *cache(rng, 1, Hkv, P, D)], [*cache(rng, B, Hkv, T, D), *cache(rng, B, Hkv, T, D)]
+    prefix[0].fill_(64), prefix[1].fill_(1.0)
+    q = torch.full((B, Hq, 1, D), -(2.0 ** 97), dtype=BF16)
+    lens = torch.zeros(B, dtype=I32)
+    want, bound = reference(q, prefix, own, lens, 0.125)
+    got = sa.slim_attn_decode_int8_shared_prefix(q.cuda(), *on_gpu(prefix), *on_gpu(own), lens.cuda(), 0.125)
+    assert ((got.double().cpu() - want).abs() <= bound).all()
+
+
+@gpu
 def test_shared_prefix_lengths_out_of_range_and_repeats(sa):
     """Lengths are taken as the nearest bound; ten calls give the same bits, on two streams at once with a workspace each."""
     rng = np.random.default_rng(4)

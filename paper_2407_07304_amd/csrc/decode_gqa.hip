@@ -30,11 +30,26 @@
 // workgroups, the combine kernel of decode.hip merges them in fixed order.
 #include <type_traits>
 
-#include "decode_sweep.h"
 #include "slim_common.h"
 #include "slim_kernels.h"
 
 namespace slim {
+
+constexpr int kGqaTile = 32;    // tokens per tile
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x2 __attribute__((ext_vector_type(2)));
+typedef __attribute__((address_space(3))) i32x2 lds_i32x2;
+
+// 8 INT8 codes -> 8 bf16, exact
+__device__ __forceinline__ bf16x8 widen8(const i32x2 cw) {
+    u32x4 r;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+        r[2 * e] = pack_bf16x2(i8_to_f32<0>(cw[e]), i8_to_f32<1>(cw[e]));
+        r[2 * e + 1] = pack_bf16x2(i8_to_f32<2>(cw[e]), i8_to_f32<3>(cw[e]));
+    }
+    return __builtin_bit_cast(bf16x8, r);
+}
 
 // D head dimension, W waves per workgroup, NC groups of 16 heads.
 // TRAFFIC_ONLY: the measurement form of the kernel (include/slimprobe.h): the same workgroups, waves, token runs and
@@ -51,10 +66,21 @@ __global__ __launch_bounds__(64 * W) void slim_decode_int8_gqa_kernel(
     const int8_t* __restrict__ vc, const float* __restrict__ vs, uint16_t* __restrict__ out, float* __restrict__ ws_acc,
     float* __restrict__ ws_ml, const int* __restrict__ kv_lens, int G, int Hkv, int T_alloc, int n_split,
     unsigned split_rate, int mode, float scale_log2e) {
-    constexpr int WAVE_BYTES = GqaLds<D, NC>::WAVE_BYTES;
+    constexpr int KS = D / 64;            // 16-byte pieces of a K row per lane (two k-steps of the score MFMA each)
+    constexpr int DT = D / 16;            // 16-row tiles of O^T
+    constexpr int CPR = D / 16;           // 16-byte pieces per row
+    constexpr int NP = kGqaTile * CPR / 64;   // 128-bit loads per lane, tile and tensor
+    constexpr int PITCH = D + 16;         // LDS row pitch: 16 rows' pieces of a read fall on 16 different groups of four banks
+    constexpr int TILE = kGqaTile * PITCH;
+    constexpr int WAVE_LDS = 2 * TILE + 256;   // K tile, V tile, the tile's 32 + 32 scales
+    constexpr int OPITCH = D + 4;         // floats per head in a wave's merge record (behind its maxima and sums)
+    constexpr int MERGE_LDS = 16 * NC * (OPITCH + 2) * 4;
+    constexpr int WAVE_BYTES = WAVE_LDS > MERGE_LDS ? WAVE_LDS : MERGE_LDS;
+
     __shared__ __attribute__((aligned(16))) char smem[W * WAVE_BYTES];
 
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));   // (the wave index as a scalar: everything derived from it stays uniform)
+    const int l16 = lane & 15, lq = lane >> 4;
     const int Hq = G * Hkv;   // (G query heads per KV head)
     int g = blockIdx.y, b = blockIdx.z, T;
     const int sp = blockIdx.x;
@@ -67,6 +93,8 @@ __global__ __launch_bounds__(64 * W) void slim_decode_int8_gqa_kernel(
         T = kv_lens ? min(max(kv_lens[b], 1), T_alloc) : T_alloc;
     }
     char* const kS = smem + w * WAVE_BYTES;
+    char* const vS = kS + TILE;
+    float* const scS = reinterpret_cast<float*>(kS + 2 * TILE);   // [0,32) k_scale * c, [32,64) v_scale
 
     // T_alloc is the cache's allocated length (the row stride); this sequence's first T tokens count.  The sequence's
     // own tiles are dealt evenly over its splits, and a split's tiles to its waves in turn.
@@ -79,18 +107,216 @@ __global__ __launch_bounds__(64 * W) void slim_decode_int8_gqa_kernel(
     first += w;
     const int n_tiles = first < end ? (end - first + W - 1) / W : 0;
 
-    f32x4 o[NC][D / 16];
-    float M[NC], lsum[NC];
-    // (a column past the last head: the last head again)
-    gqa_sweep<D, W, NC, TRAFFIC_ONLY>(kS, lane, [&](int i) { return q + ((long)b * Hq + (long)g * G + min(i, G - 1)) * D; }, kc + kvrow0 * D,
-                                      ks + kvrow0, vc + kvrow0 * D, vs + kvrow0, T, first, n_tiles, scale_log2e,
-                                      [](int, int, const float (&)[8]) {}, o, M, lsum);
-    gqa_record<D, NC>(kS, lane, o, M, lsum);
+    // Q^T B operands: lane holds head l16 of its group of 16 (a column past the last head: the last head again),
+    // d = 64 s + 16 lq + 8 e + [0,8)
+    bf16x8 qB[NC][KS][2];
+#pragma unroll
+    for (int nc = 0; nc < NC; ++nc) {
+        const uint16_t* qp = q + ((long)b * Hq + (long)g * G + min(16 * nc + l16, G - 1)) * D + 16 * lq;
+#pragma unroll
+        for (int s = 0; s < KS; ++s)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) qB[nc][s][e] = *reinterpret_cast<const bf16x8*>(qp + 64 * s + 8 * e);
+    }
+
+    // Piece lane + 64 n of a tile (row-major, 16 codes each), through buffer descriptors that cover exactly this
+    // (batch, KV head)'s slab: rows past the end of the cache read as zero (and are masked) and a load costs one
+    // vector add.  The codes are used once: non-temporal.
+    const __amdgpu_buffer_rsrc_t krs = __builtin_amdgcn_make_buffer_rsrc((void*)(kc + kvrow0 * D), 0, (int)((unsigned)T * D), 0x00020000);
+    const __amdgpu_buffer_rsrc_t vrs = __builtin_amdgcn_make_buffer_rsrc((void*)(vc + kvrow0 * D), 0, (int)((unsigned)T * D), 0x00020000);
+    // (the scales through descriptors as well: lanes 0-31 want the K scale of token lane, lanes 32-63 the V scale; each
+    // load asks the other half's lanes for an offset past the end, which reads nothing, so a tile's loads are the
+    // same instructions whether the tile is wanted or not)
+    const __amdgpu_buffer_rsrc_t ksr = __builtin_amdgcn_make_buffer_rsrc((void*)(ks + kvrow0), 0, (int)((unsigned)T * 4u), 0x00020000);
+    const __amdgpu_buffer_rsrc_t vsr = __builtin_amdgcn_make_buffer_rsrc((void*)(vs + kvrow0), 0, (int)((unsigned)T * 4u), 0x00020000);
+    const bool k_half = lane < 32;
+    const int s_off_k = k_half ? lane * 4 : (int)0x7ffffff0, s_off_v = k_half ? (int)0x7ffffff0 : (lane - 32) * 4;
+    u32x4 kbuf[NP], vbuf[NP];
+    float sc = 0.0f;
+    auto issue = [&](const __amdgpu_buffer_rsrc_t rs, u32x4 (&buf)[NP], int t0) {
+#pragma unroll
+        for (int n = 0; n < NP; ++n) buf[n] = __builtin_amdgcn_raw_buffer_load_b128(rs, lane * 16 + n * 1024 + t0 * D, 0, 2 /* nt */);
+    };
+    auto issue_k = [&](int t0) {
+        issue(krs, kbuf, t0);
+        const uint32_t a = __builtin_amdgcn_raw_buffer_load_b32(ksr, s_off_k + t0 * 4, 0, 0);
+        const uint32_t c = __builtin_amdgcn_raw_buffer_load_b32(vsr, s_off_v + t0 * 4, 0, 0);
+        sc = __builtin_bit_cast(float, a | c);   // (the lanes a load left out received zero)
+    };
+    auto issue_v = [&](int t0) { issue(vrs, vbuf, t0); };
+    auto stage = [&](const u32x4 (&buf)[NP], char* tile) {   // a tile's codes into LDS
+#pragma unroll
+        for (int n = 0; n < NP; ++n)
+            *reinterpret_cast<u32x4*>(tile + ((lane + 64 * n) / CPR) * PITCH + (lane % CPR) * 16) = buf[n];
+    };
+
+    // Every load of the kernel is issued unconditionally: a tile that is not wanted (past the end of this wave's
+    // run) is asked for at token T, past the end of the descriptor, so zeros arrive and no memory is read.  The
+    // compiler places a wait by counting the loads issued after the one it needs, along the worst path that leads
+    // there; loads under a branch are not outstanding on the path that skips them, and at the loop's head the
+    // worst path may be the one from the prologue.  So the prologue's four groups keep the order the loop issues
+    // them in (K, V of a tile, then the next tile's).
+    auto t_of = [&](int i) { return i < n_tiles ? (first + i * W) * kGqaTile : T; };
+    __builtin_amdgcn_sched_barrier(0);
+    issue_k(t_of(0));
+    __builtin_amdgcn_sched_barrier(0);
+    issue_v(t_of(0));
+    __builtin_amdgcn_sched_barrier(0);
+
+    // K fragments of token tile tt, k-steps 2 s and 2 s + 1: row 16 tt + l16, bytes 64 s + 16 lq + [0,16).  V^T fragment of tile dt: the
+    // 16 lanes of a group fetch 8 rows (2 lanes a row, 8 columns each) and lane j of the group receives column j of
+    // them; the rows of group lq are the tokens its probabilities belong to: 4 lq + [0,4) and 16 + 4 lq + [0,4).
+    const int k_addr = l16 * PITCH + 16 * lq;
+    const int v_row = l16 >> 1;
+    const int v_addr = (4 * lq + (v_row & 3) + 16 * (v_row >> 2)) * PITCH + 8 * (l16 & 1);
+
+    f32x4 o[NC][DT];
+    float M[NC], lsum[NC];   // running max of this lane's head (log2 units), this lane's part of the row sum
+#pragma unroll
+    for (int nc = 0; nc < NC; ++nc) {
+        M[nc] = kMasked;
+        lsum[nc] = 0.0f;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) o[nc][dt] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+
+    for (int i = 0; i < n_tiles; ++i) {
+        const int t0 = t_of(i);
+        const int t_next = t_of(i + 1);
+        if constexpr (TRAFFIC_ONLY) {
+            u32x4 x = {0u, 0u, 0u, 0u};
+#pragma unroll
+            for (int n = 0; n < NP; ++n) x ^= kbuf[n] ^ vbuf[n];
+            lsum[0] += __uint_as_float((x[0] ^ x[1] ^ x[2] ^ x[3]) & 0x3fffffffu) + sc;
+            issue_k(t_next);
+            issue_v(t_next);
+            // (each tile is consumed and refilled on its own, as in the full kernel: without this the compiler
+            // folds the two tiles of a pair into one sum and waits for both at once)
+            asm volatile("" : "+v"(lsum[0]));
+            __builtin_amdgcn_sched_barrier(0);
+            continue;
+        }
+
+        stage(kbuf, kS);
+        scS[lane] = k_half ? sc * scale_log2e : sc;
+        issue_k(t_next);
+        i32x4 kw[2][KS];
+#pragma unroll
+        for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+            for (int s = 0; s < KS; ++s) kw[tt][s] = *reinterpret_cast<const i32x4*>(kS + k_addr + 16 * tt * PITCH + 64 * s);
+        __builtin_amdgcn_sched_barrier(0);
+        stage(vbuf, vS);
+        issue_v(t_next);
+        __builtin_amdgcn_sched_barrier(0);
+
+        // scores: register r of token tile tt is token 16 tt + 4 lq + r, column = head l16 of the group
+        bf16x8 kf[2][KS][2];
+#pragma unroll
+        for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+            for (int s = 0; s < KS; ++s) {
+                kf[tt][s][0] = widen8(i32x2{kw[tt][s][0], kw[tt][s][1]});
+                kf[tt][s][1] = widen8(i32x2{kw[tt][s][2], kw[tt][s][3]});
+            }
+        u32x4 pw[NC];
+#pragma unroll
+        for (int nc = 0; nc < NC; ++nc) {
+            f32x4 acc[2] = {{0.0f, 0.0f, 0.0f, 0.0f}, {0.0f, 0.0f, 0.0f, 0.0f}};
+#pragma unroll
+            for (int s = 0; s < KS; ++s)
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+#pragma unroll
+                    for (int tt = 0; tt < 2; ++tt)
+                        acc[tt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[tt][s][e], qB[nc][s][e], acc[tt], 0, 0, 0);
+            float u[8];
+#pragma unroll
+            for (int tt = 0; tt < 2; ++tt) {
+                const f32x4 kf4 = *reinterpret_cast<const f32x4*>(&scS[16 * tt + 4 * lq]);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) u[4 * tt + r] = acc[tt][r] * kf4[r];
+            }
+            if (t0 + kGqaTile > T) {   // the sequence ends inside this tile (or before it)
+#pragma unroll
+                for (int r = 0; r < 8; ++r) u[r] = (t0 + 16 * (r / 4) + 4 * lq + r % 4 < T) ? u[r] : kMasked;
+            }
+            float umax = fmaxf(u[0], u[1]);
+#pragma unroll
+            for (int r = 2; r < 8; r += 2) umax = fmaxf(umax, fmaxf(u[r], u[r + 1]));
+            // the running max moves only when a score has passed it by 2^8 (always on a wave's first tile)
+            if (__builtin_amdgcn_ballot_w64(umax - M[nc] > 8.0f) != 0) {
+                float m_new = fmaxf(M[nc], umax);
+                m_new = fmaxf(m_new, __shfl_xor(m_new, 16));
+                m_new = ceilf(fmaxf(m_new, __shfl_xor(m_new, 32)));
+                const float alpha = fast_exp2(M[nc] - m_new);
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt) o[nc][dt] *= alpha;
+                lsum[nc] *= alpha;
+                M[nc] = m_new;
+            }
+            float ps0 = 0.0f, ps1 = 0.0f;
+#pragma unroll
+            for (int r = 0; r < 8; r += 2) {
+                u[r] = fast_exp2(u[r] - M[nc]);
+                u[r + 1] = fast_exp2(u[r + 1] - M[nc]);
+                ps0 += u[r];
+                ps1 += u[r + 1];
+            }
+            lsum[nc] += ps0 + ps1;
+            // the probabilities take their token's v_scale before they are rounded to bf16
+#pragma unroll
+            for (int tt = 0; tt < 2; ++tt) {
+                const f32x4 vf = *reinterpret_cast<const f32x4*>(&scS[32 + 16 * tt + 4 * lq]);
+                pw[nc][2 * tt] = pack_bf16x2(u[4 * tt] * vf[0], u[4 * tt + 1] * vf[1]);
+                pw[nc][2 * tt + 1] = pack_bf16x2(u[4 * tt + 2] * vf[2], u[4 * tt + 3] * vf[3]);
+            }
+        }
+
+        // O^T += V^T P^T over the tile's 32 tokens: element j of lane group lq is token 4 lq + j (j < 4) or 16 + 4 lq + j - 4
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) {
+            const i32x2 vw = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2*)(vS + v_addr + 16 * dt));
+            const bf16x8 va = widen8(vw);
+#pragma unroll
+            for (int nc = 0; nc < NC; ++nc)
+                o[nc][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, __builtin_bit_cast(bf16x8, pw[nc]), o[nc][dt], 0, 0, 0);
+        }
+    }
+
+    // Merge the waves: register r of tile dt is d = 16 dt + 4 lq + r of head l16.  A wave's record: 16 NC maxima (log2
+    // units), as many sums, then the accumulators, a row of OPITCH floats per head (over its own tiles, which are dead).
+    float* const rec = reinterpret_cast<float*>(kS);
+#pragma unroll
+    for (int nc = 0; nc < NC; ++nc) {
+        float L = lsum[nc];
+        L += __shfl_xor(L, 16);
+        L += __shfl_xor(L, 32);
+        if (lq == 0) {
+            rec[16 * nc + l16] = M[nc];
+            rec[16 * NC + 16 * nc + l16] = L;
+        }
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+            *reinterpret_cast<f32x4*>(rec + 32 * NC + (16 * nc + l16) * OPITCH + 16 * dt + 4 * lq) = o[nc][dt];
+    }
     __syncthreads();
     for (int x = threadIdx.x; x < G * D; x += 64 * W) {
         const int h = x / D, d = x % D;
-        float acc, top, L;
-        gqa_merged<D, W, NC>(smem, h, d, acc, top, L);
+        float m[W], top = kMasked;
+#pragma unroll
+        for (int ww = 0; ww < W; ++ww) {
+            m[ww] = reinterpret_cast<const float*>(smem + ww * WAVE_BYTES)[h];
+            top = ww == 0 ? m[ww] : fmaxf(top, m[ww]);
+        }
+        float L = 0.0f, acc = 0.0f;
+#pragma unroll
+        for (int ww = 0; ww < W; ++ww) {
+            const float* r = reinterpret_cast<const float*>(smem + ww * WAVE_BYTES);
+            const float f = fast_exp2(m[ww] - top);   // a wave without tiles has L = 0 and an accumulator of zeros
+            L = fmaf(f, r[16 * NC + h], L);
+            acc = fmaf(f, r[32 * NC + h * OPITCH + d], acc);
+        }
         const long bh = (long)b * Hq + (long)g * G + h;
         if (!TRAFFIC_ONLY && n_used == 1) {   // (the measurement form has a workspace only)
             out[bh * D + d] = (uint16_t)(pack_bf16x2(acc / L, 0.0f) & 0xffffu);

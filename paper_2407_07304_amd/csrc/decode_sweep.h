@@ -1,5 +1,6 @@
-// What the decode kernels over the INT8 cache share: the sweep of a run of a KV head's tokens for several rows of queries on the
-// matrix cores, the merge of a workgroup's waves, and the merge of the records that several workgroups leave.
+// What decode kernels over the INT8 cache share: the sweep of a run of a KV head's tokens for several rows of queries on the matrix
+// cores and the merge of a workgroup's waves (the grouped decode's; decode_gqa.hip, which explains them, has them written out: inlined from
+// here, the same steps take that kernel 4 % less to 4 % more, shape by shape), and the merge of the records that workgroups leave.
 #pragma once
 #include "slim_common.h"
 
@@ -40,7 +41,7 @@ struct GqaLds {
 // column i's row of D query values.  Out: running max of this lane's column (log2 units), this lane's part of its sum, the
 // accumulators.  keep(nc, t0, u): sees the scores (log2 units; register 4 tt + r is token t0 + 16 tt + 4 lq + r) of every tile.
 // kS: the wave's own LDS.
-template <int D, int W, int NC, bool TRAFFIC_ONLY, class QRow, class Keep>
+template <int D, int W, int NC, class QRow, class Keep>
 __device__ __forceinline__ void gqa_sweep(char* const kS, const int lane, const QRow q_row, const int8_t* kc, const float* ks, const int8_t* vc,
                                           const float* vs, const int T, const int first, const int n_tiles, const float scale_log2e,
                                           const Keep keep, f32x4 (&o)[NC][D / 16], float (&M)[NC], float (&lsum)[NC]) {
@@ -127,19 +128,6 @@ __device__ __forceinline__ void gqa_sweep(char* const kS, const int lane, const 
     for (int i = 0; i < n_tiles; ++i) {
         const int t0 = t_of(i);
         const int t_next = t_of(i + 1);
-        if constexpr (TRAFFIC_ONLY) {
-            u32x4 x = {0u, 0u, 0u, 0u};
-#pragma unroll
-            for (int n = 0; n < NP; ++n) x ^= kbuf[n] ^ vbuf[n];
-            lsum[0] += __uint_as_float((x[0] ^ x[1] ^ x[2] ^ x[3]) & 0x3fffffffu) + sc;
-            issue_k(t_next);
-            issue_v(t_next);
-            // (each tile is consumed and refilled on its own, as in the full kernel: without this the compiler
-            // folds the two tiles of a pair into one sum and waits for both at once)
-            asm volatile("" : "+v"(lsum[0]));
-            __builtin_amdgcn_sched_barrier(0);
-            continue;
-        }
 
         stage(kbuf, kS);
         scS[lane] = k_half ? sc * scale_log2e : sc;

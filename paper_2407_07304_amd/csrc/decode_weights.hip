@@ -94,7 +94,7 @@ __global__ __launch_bounds__(64 * W) void slim_decode_weights_kernel(const Weigh
 
     f32x4 o[NC][D / 16];
     float M[NC], lsum[NC];
-    gqa_sweep<D, W, NC, false>(kS, lane, [&](int i) { return p.q + (row0 + min(i, heads - 1)) * D; }, p.kc + kvrow0 * D, p.ks + kvrow0,
+    gqa_sweep<D, W, NC>(kS, lane, [&](int i) { return p.q + (row0 + min(i, heads - 1)) * D; }, p.kc + kvrow0 * D, p.ks + kvrow0,
                                p.vc + kvrow0 * D, p.vs + kvrow0, T, first, first < end ? (end - first + W - 1) / W : 0, p.scale_log2e,
                                [&](int nc, int t0, const float (&u)[8]) {
                                    // (through a descriptor over the tile's rows: the columns past the last head store nothing, and the store is the

@@ -30,7 +30,7 @@ template <int D>
 struct PrefixLds {
     static constexpr int STAGE = 64;
     static constexpr int PITCHK = 2 * D + 16, PITCHV = 2 * D + 64;
-    static constexpr int STAGE_BYTES = STAGE * (PITCHK + PITCHV) + 8 * STAGE;
+    static constexpr int STAGE_BYTES = STAGE * (PITCHK + PITCHV) + 16 * STAGE;   // (64 floats a wave, of which two have something to say)
     static constexpr int BYTES = 2 * STAGE_BYTES;
 };
 
@@ -71,30 +71,34 @@ __device__ __forceinline__ void prefix_sweep(char* const smem, const QRow q_row,
     auto issue = [&](auto set_c, int t0) __attribute__((always_inline)) {
         constexpr int set = decltype(set_c)::value;
         const int base = t0 < t_end ? t0 : T;          // (a stage that is not wanted: nothing is read)
+        sc[set] = __builtin_amdgcn_raw_buffer_load_b32(srs, (base + lane) * 4, 0, 0);
         const int off = (int)((unsigned)base * D + (unsigned)(tid * 16));
 #pragma unroll
         for (int n = 0; n < NP; ++n) buf[set][0][n] = __builtin_amdgcn_raw_buffer_load_b128(krs, off + n * 4096, 0, 0);
 #pragma unroll
         for (int n = 0; n < NP; ++n) buf[set][1][n] = __builtin_amdgcn_raw_buffer_load_b128(vrs, off + n * 4096, 0, 0);
-        sc[set] = __builtin_amdgcn_raw_buffer_load_b32(srs, (base + lane) * 4, 0, 0);
     };
+    const int tile0 = NT == 1 ? 32 * phase : 0;  // of the stage
+    // Addresses in a buffer, K's, V's and the scales' (the compiler sees no constant in them: it would add it to a buffer's offset, more than
+    // the 16 bits of an instruction, and keep a register for every sum, when there is none to spare)
+    int k_addr = (tile0 + l32) * PITCHK + 16 * hh;   // K fragment of k-step s: row l32, bytes 32 s + 16 hh + [0,16)
+    // V transpose reads: 16 lanes fetch rows k..k+3, lane i receives column i of them
+    int v_addr = STAGE * PITCHK + (tile0 + 4 * hh + ((lane & 15) >> 2)) * PITCHV + (2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) * 16 + 8 * (lane & 1);
+    int s_addr = STAGE * (PITCHK + PITCHV) + 4 * (tile0 + 4 * hh);
+    int k_to = tid * 16 / D * PITCHK + tid * 16 % D * 2, v_to = STAGE * PITCHK + tid * 16 / D * PITCHV + tid * 16 % D * 2;
+    int s_to = STAGE * (PITCHK + PITCHV) + 4 * tid;
+    asm("" : "+v"(k_addr), "+v"(v_addr), "+v"(s_addr), "+v"(k_to), "+v"(v_to), "+v"(s_to));
     // piece i of a stage on its way into LDS: 8 codes of K (the first half) or V -> 8 bf16, exact
     auto piece = [&](int set, char* to, int i) __attribute__((always_inline)) {
         const int x = i / (2 * NP), n = i / 2 % NP, half = i % 2;
-        const int at = tid * 16 + n * 4096, row = at / D, col = at % D;
-        char* const dst = to + (x == 0 ? row * PITCHK : STAGE * PITCHK + row * PITCHV) + col * 2 + 16 * half;
+        char* const dst = to + (x == 0 ? k_to : v_to) + 4096 / D * n * (x == 0 ? PITCHK : PITCHV) + 16 * half;
         *reinterpret_cast<bf16x8*>(dst) = widen8(i32x2{(int)buf[set][x][n][2 * half], (int)buf[set][x][n][2 * half + 1]});
     };
+    const float scale_by = w == 0 ? scale_log2e : 1.0f;
     auto scales = [&](int set, char* to) __attribute__((always_inline)) {   // [0, STAGE) k_scale * c, then v_scale
-        float* const scS = reinterpret_cast<float*>(to + STAGE * (PITCHK + PITCHV));
-        const float s = __uint_as_float(sc[set]);
-        if (w < 2) scS[64 * w + lane] = w == 0 ? s * scale_log2e : s;
+        *reinterpret_cast<float*>(to + s_to) = __uint_as_float(sc[set]) * scale_by;
     };
 
-    const int tile0 = NT == 1 ? 32 * phase : 0;  // of the stage
-    const int k_addr = (tile0 + l32) * PITCHK + 16 * hh;   // K fragment of k-step s: row l32, bytes 32 s + 16 hh + [0,16)
-    // V transpose reads: 16 lanes fetch rows k..k+3, lane i receives column i of them
-    const int v_addr = STAGE * PITCHK + (tile0 + 4 * hh + ((lane & 15) >> 2)) * PITCHV + (2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) * 16 + 8 * (lane & 1);
     f32x16 o[DT];
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
@@ -105,12 +109,21 @@ __device__ __forceinline__ void prefix_sweep(char* const smem, const QRow q_row,
 
     const std::integral_constant<int, 0> set0{};
     const std::integral_constant<int, 1> set1{};
+    // (The compiler waits for a load by counting those issued behind it, on the path that has fewest: here they come in the order in which the
+    // loop issues them, none is under a branch, and the loop, which has two stages, is not left between them; an odd number's last one is
+    // all mask.  Where one of the three was not so, every other stage waited for its successor's loads: 64 on 8 heads, 20 sequences,
+    // P=32768 57.8 us and 52.2, 32 on 8, 64 sequences, P=2048 21.6 and 20.0.)
+    __builtin_amdgcn_sched_barrier(0);
     issue(set0, t_begin);
+    __builtin_amdgcn_sched_barrier(0);
     issue(set1, t_begin + STAGE);
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int i = 0; i < KS; ++i) piece(0, smem, i);
     scales(0, smem);
+    __builtin_amdgcn_sched_barrier(0);
     issue(set0, t_begin + 2 * STAGE);
+    __builtin_amdgcn_sched_barrier(0);
     __syncthreads();
     // the stage from token t0 on, in LDS buffer `turn`; the one behind it goes into the other, which every wave is done with since the
     // last barrier
@@ -118,7 +131,7 @@ __device__ __forceinline__ void prefix_sweep(char* const smem, const QRow q_row,
         constexpr int turn = decltype(turn_c)::value;
         const char* const kS = smem + turn * Lds::STAGE_BYTES;
         char* const next = smem + (turn ^ 1) * Lds::STAGE_BYTES;
-        const float* const scS = reinterpret_cast<const float*>(kS + STAGE * (PITCHK + PITCHV)) + tile0 + 4 * hh;
+        const float* const scS = reinterpret_cast<const float*>(kS + s_addr);
         scales(turn ^ 1, next);
         f32x16 u[NT];
 #pragma unroll
@@ -160,17 +173,17 @@ __device__ __forceinline__ void prefix_sweep(char* const smem, const QRow q_row,
 #pragma unroll
             for (int i = 0; i < 2; ++i) vscale[x & 1][i] = *reinterpret_cast<const f32x4*>(scS + STAGE + 16 * x + 8 * i);
         };
-        fetch_scales(0);
-        fetch_scales(1);
-        fetch_v(0);
-        __builtin_amdgcn_sched_barrier(0);
         // register r of u[t] is token t0 + tile0 + 32 t + 8 (r/4) + 4 hh + r%4; scores relative to the running max
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
             for (int r = 0; r < 16; ++r) u[t][r] = fmaf(u[t][r], kscale[t][r / 4][r % 4], -M);
         __builtin_amdgcn_sched_barrier(0);
+        fetch_scales(0);
+        fetch_scales(1);
+        fetch_v(0);
         issue(std::integral_constant<int, turn ^ 1>{}, t0 + 3 * STAGE);   // (here, where registers are free again)
+        __builtin_amdgcn_sched_barrier(0);
         if (t0 + STAGE > T) {
 #pragma unroll
             for (int t = 0; t < NT; ++t)
@@ -231,11 +244,9 @@ __device__ __forceinline__ void prefix_sweep(char* const smem, const QRow q_row,
         lsum += ps;
         __syncthreads();
     };
-    for (int t0 = t_begin;; t0 += 2 * STAGE) {   // (at least one stage)
+    for (int t0 = t_begin; t0 < t_end; t0 += 2 * STAGE) {
         work(set0, t0);
-        if (t0 + STAGE >= t_end) break;
         work(set1, t0 + STAGE);
-        if (t0 + 2 * STAGE >= t_end) break;
     }
     const float L = half_sum(lsum);
     const int row = 32 * rg + l32;
@@ -290,9 +301,9 @@ __global__ __launch_bounds__(256, 2) void slim_decode_prefix_kernel(const Prefix
         if constexpr (FORM >= 3) {
             constexpr int STAGE = PrefixLds<D>::STAGE, PHASES = 4 / RG;
             int first, end;
-            split_span((p.P + STAGE - 1) / STAGE, p.n_prefix / PHASES, sp, first, end);
+            split_span((p.P + 2 * STAGE - 1) / (2 * STAGE), p.n_prefix / PHASES, sp, first, end);
             prefix_sweep<D, RG>(smem, [&](int i) { return p.q + row_of(i) * D; }, n_rows, p.pkc + kv0 * D, p.pks + kv0, p.pvc + kv0 * D,
-                                p.pvs + kv0, p.P, first * STAGE, min(end * STAGE, p.P), p.scale_log2e,
+                                p.pvs + kv0, p.P, first * 2 * STAGE, min(end * 2 * STAGE, p.P), p.scale_log2e,
                                 [&](int i, int phase) { return row_of(i) * p.n_records + sp * PHASES + phase; }, p.ws_acc, p.ws_ml);
         } else {
             int first, end;
@@ -363,10 +374,10 @@ static PrefixPlan prefix_plan(int batch, int q_heads, int kv_heads, int prefix_l
     plan.row_blocks = (int)((rows + 127) / 128);
     plan.head_groups = (G + 31) / 32;
     // The prefix: a workgroup a compute unit, beside which there is room for one of an own cache, or two where each still has 32 stages
-    // (64 on 8 heads, 64 sequences, P=32768 104.6 and 93.1 us); and none with less than 4 stages, 8 from 2048
-    // query rows on, as every one costs a record of its rows besides (32 on 8 heads, 48 sequences, P=1024, T=100 with 1, 4 and 8 stages 21.3,
-    // 14.8 and 19.6 us; 64 on 8 heads, 128 sequences, P=512 27.0, 22.8 and 23.7; 32 heads, 128 sequences, P=2000 44.6, 44.6 and 38.9).  Up to 32
-    // rows a record is little: two tiles a wave (32 on 8 heads, 2 sequences, P=4000, T=100 14.0 us with 8, 11.0 with 4, 9.5).
+    // (64 on 8 heads, 64 sequences, P=32768 107 and 93 us); and none with less than 4 stages, 8 from 2048 query rows on, as every one
+    // costs a record of its rows besides (with 4, 8 and 16 stages 32 on 8 heads, 48 sequences, P=1024, T=100 14.3, 18.6 and 27.9 us; 128
+    // sequences, P=2000 27.8, 21.2 and 29.3; 32 heads, 128 sequences, P=2000 43.7, 38.3 and 36.6).  Up to 32 rows a record is little: two
+    // tiles a wave (32 on 8 heads, 2 sequences, P=4000, T=100 14.0 us with 8, 11.0 with 4, 9.5).
     const int phases = plan.form == 3 ? 2 : 1;
     const long items = (long)kv_heads * plan.row_blocks, stages = ((long)prefix_len + (plan.form < 3 ? 127 : 63)) / (plan.form < 3 ? 128 : 64);
     long n = (256 + items - 1) / items;

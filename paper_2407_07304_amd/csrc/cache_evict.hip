@@ -4,7 +4,8 @@
 // Two launches.  The first chooses: a workgroup for each (sequence, KV head) holds the weights in registers, as whole numbers of
 // the same order, finds the smallest one that stays by its bits, 11, 11 and 10 of them (a histogram in LDS, then the bin that the
 // count runs out in; no further where a whole bin stays), and numbers the tokens that stay with prefix sums.  Whole numbers only:
-// no order of atomics changes a result.  It is bound by its steps' latencies.  The second copies: 16 bytes a lane, a row of codes by
+// no order of atomics changes a result.  It is bound by its steps' latencies, and on long rows by the unit's instructions (8 rows of 32768
+// tokens: load 2.3 us, the histograms 4.2, 3.2 and 1, a bin 0.7 each, numbers 3.4).  The second copies: 16 bytes a lane, a row of codes by
 // D/16 adjacent lanes, and is bound by memory: 2 (D + 4) + 4 bytes a token, read and written.
 #include <type_traits>
 
@@ -82,17 +83,25 @@ __global__ __launch_bounds__(kSelectThreads) void slim_cache_select_kernel(const
             for (int e = 0; e < 4; ++e) key[c][e] = t0 + c * kSelectChunk + 4 * tid + e < among ? weight_key(v[c][e]) : 0u;
         }
     };
-    // f(key) for all of them
+    // f(key) for all of them, and for 0s that fill up a wave's last 256 (for all 4096 of a chunk's, the first histogram of 2000 tokens took
+    // 2.4 us and not 1.1: the 0s meet in one bin)
     auto each = [&](auto f) __attribute__((always_inline)) {
         for (int r = 0; r < rounds; ++r) {
             if (rounds > 1) load(r * C * kSelectChunk);
 #pragma unroll
             for (int c = 0; c < C; ++c) {
+                if ((r * C + c) * kSelectChunk + 256 * w < among) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) f(key[c][e]);
+                    for (int e = 0; e < 4; ++e) f(key[c][e]);
+                }
             }
         }
     };
+    auto clear = [&]() __attribute__((always_inline)) {
+        for (int i = tid; i < BINS; i += kSelectThreads) *reinterpret_cast<u32x4*>(hist[i]) = u32x4{0u, 0u, 0u, 0u};
+    };
+    clear();
+    if (tid == 0) listed = 0;
     load(0);
 
     int need = keep - recent, count = -1;   // tokens that stay of those that have the known bits, and how many have them
@@ -100,8 +109,7 @@ __global__ __launch_bounds__(kSelectThreads) void slim_cache_select_kernel(const
     unsigned prefix = 0u, known = 0u;       // bits of the smallest weight that stays, and which of them are known
     for (int pass = 0; pass < 3 && need > 0 && count != need; ++pass) {
         const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bins = pass == 2 ? 1024 : BINS;
-        for (int i = tid; i < BINS; i += kSelectThreads) *reinterpret_cast<u32x4*>(hist[i]) = u32x4{0u, 0u, 0u, 0u};
-        if (tid == 0 && pass == 0) listed = 0;
+        if (pass > 0) clear();
         __syncthreads();
         int* const mine = &hist[0][lane % COPIES];
         if (pass == 0) {
@@ -155,58 +163,67 @@ __global__ __launch_bounds__(kSelectThreads) void slim_cache_select_kernel(const
         count = foundS[2];
     }
     if (keep == recent) prefix = known = 0xffffffffu;   // (none of them; no weight has these bits)
-    // tokens above `prefix` stay, and the first `need` of those that have it.  Counted together, those
-    // above in the low half (a round has at most 2^16 - 2^12 tokens) and those that have it in the high one.
+    // Tokens from `prefix` on stay, where all of those that have its bits do (bits that are not known are 0 in it); else those above it and the
+    // first `need` of those that have them, counted together: those above in the low half (a round has at most 2^16 - 2^12 tokens),
+    // the others in the high one.  (One comparison a token, not two and their counts: of 8 rows of 32768 tokens' choice 3.4 us in the place of
+    // 6.1.)
     static_assert(C * kSelectChunk < 65536, "a round's counts fit 16 bits");
-    int above = 0, equal = 0;   // so far
-    for (int r = 0; r < rounds; ++r) {
-        if (rounds > 1) load(r * C * kSelectChunk);
-        int mine[C], before[C];
+    auto number = [&](auto ties_c) __attribute__((always_inline)) {
+        constexpr bool TIES = decltype(ties_c)::value;
+        int above = 0, equal = 0;   // so far
+        for (int r = 0; r < rounds; ++r) {
+            if (rounds > 1) load(r * C * kSelectChunk);
+            int mine[C], before[C];
 #pragma unroll
-        for (int c = 0; c < C; ++c) {
-            mine[c] = 0;
+            for (int c = 0; c < C; ++c) {
+                mine[c] = 0;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const unsigned k = key[c][e] & known;
-                mine[c] += k > prefix ? 1 : k == prefix ? 65536 : 0;
+                for (int e = 0; e < 4; ++e)
+                    mine[c] += TIES ? (key[c][e] > prefix ? 1 : key[c][e] == prefix ? 65536 : 0) : key[c][e] >= prefix;
+                before[c] = wave_prefix(mine[c]);
+                if (lane == 63) groupS[c * kSelectWaves + w] = before[c];
+                before[c] -= mine[c];
             }
-            before[c] = wave_prefix(mine[c]);
-            if (lane == 63) groupS[c * kSelectWaves + w] = before[c];
-            before[c] -= mine[c];
-        }
-        __syncthreads();
-        // every wave: lane l has groups 4 l to 4 l + 3 (in the order of their tokens)
-        int of[4], sum = 0;
+            __syncthreads();
+            // every wave: lane l has groups 4 l to 4 l + 3 (in the order of their tokens)
+            int of[4], sum = 0;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            of[i] = 4 * lane + i < GROUPS ? groupS[4 * lane + i] : 0;
-            sum += of[i];
-        }
-        const int incl = wave_prefix(sum);
-        int base = incl - sum;   // before this lane's group of this wave's number: those of the lanes before, and of its own
+            for (int i = 0; i < 4; ++i) {
+                of[i] = 4 * lane + i < GROUPS ? groupS[4 * lane + i] : 0;
+                sum += of[i];
+            }
+            const int incl = wave_prefix(sum);
+            int base = incl - sum;   // before this lane's group of this wave's number: those of the lanes before, and of its own
 #pragma unroll
-        for (int i = 0; i < 3; ++i) base += i < (w & 3) ? of[i] : 0;
+            for (int i = 0; i < 3; ++i) base += i < (w & 3) ? of[i] : 0;
 #pragma unroll
-        for (int c = 0; c < C; ++c) {
-            before[c] += __builtin_amdgcn_readlane(base, (c * kSelectWaves + w) >> 2);
-            if (mine[c] != 0) {
-                int na = above + (before[c] & 0xffff), ne = equal + (int)((unsigned)before[c] >> 16);
+            for (int c = 0; c < C; ++c) {
+                before[c] += __builtin_amdgcn_readlane(base, (c * kSelectWaves + w) >> 2);
                 const int t = (r * C + c) * kSelectChunk + 4 * tid;
+                if constexpr (TIES) {
+                    int na = above + (before[c] & 0xffff), ne = equal + (int)((unsigned)before[c] >> 16);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const unsigned k = key[c][e] & known;
-                    const bool up = k > prefix, eq = k == prefix;
-                    if (up || (eq && ne < need)) to[na + min(ne, need)] = t + e;
-                    na += up;
-                    ne += eq;
+                    for (int e = 0; e < 4; ++e) {
+                        const bool up = key[c][e] > prefix, eq = key[c][e] == prefix;
+                        if (up || (eq && ne < need)) to[na + min(ne, need)] = t + e;
+                        na += up;
+                        ne += eq;
+                    }
+                } else {
+                    unsigned at = (unsigned)(above + before[c]);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (key[c][e] >= prefix) to[at++] = t + e;
                 }
             }
+            const int total = __builtin_amdgcn_readlane(incl, 63);
+            above += total & 0xffff;
+            equal += (int)((unsigned)total >> 16);
+            __syncthreads();
         }
-        const int total = __builtin_amdgcn_readlane(incl, 63);
-        above += total & 0xffff;
-        equal += (int)((unsigned)total >> 16);
-        __syncthreads();
-    }
+    };
+    if (count != need && keep != recent) number(std::true_type{});   // (then all the bits are known)
+    else number(std::false_type{});
     for (int i = tid; i < recent; i += kSelectThreads) to[keep - recent + i] = among + i;
 }
 

@@ -296,6 +296,20 @@ def test_eviction_of_many_near_weights(sa, T, spread):
 
 
 @gpu
+@pytest.mark.parametrize("kind", ["ties", "nan"])
+def test_eviction_of_lengths_about_a_chunk(sa, kind):
+    """Lengths (without the recent tokens) one token either side of a wave's, a chunk's and a round's, in caches of more."""
+    rng = np.random.default_rng(23)
+    for T, edges in ((9000, (256, 4096, 4096 + 256, 8192)), (38000, (32768, 32768 + 4096))):
+        lens = np.array([e + 7 + d for e in edges for d in (-1, 0, 1)], np.int32)
+        w = (rng.random((len(lens), 1, T)) * 8).round().astype(np.float32)
+        if kind == "nan":
+            w[rng.random(w.shape) < 0.5] = np.nan
+        for keep in (8, 100, 200):
+            check_evict(sa, rng, len(lens), 1, 64, T, keep, 7, keep, w, lens, "%s T%d keep%d" % (kind, T, keep))
+
+
+@gpu
 def test_eviction_replays_from_a_graph(sa):
     rng = np.random.default_rng(12)
     B, Hkv, T, D, keep, recent = 4, 2, 3000, 128, 1000, 64

@@ -95,6 +95,20 @@ __global__ __launch_bounds__(256) void slim_qk_norm_rope_kernel(const RopeArgs p
         const int b = (int)(token / p.seq_len), s = (int)(token - (long)b * p.seq_len);
         const int u_end = min((part + 1) * per_part, uq + 2 * uk);
 
+        // unit u's kind (uniform), and this lane's head of it: past the last one that head's again, which is not stored
+        auto unit = [&](int u, int& kind, int& heads, int& h) {
+            kind = u < uq ? 0 : u < uq + uk ? 1 : 2;
+            heads = kind == 0 ? p.q_heads : p.kv_heads;
+            h = (u - (kind == 0 ? 0 : kind == 1 ? uq : uq + uk)) * RW + sub;
+        };
+        auto load = [&](int u) {
+            int kind, heads, h;
+            unit(u, kind, heads, h);
+            return load_piece<D, PAIRS>((const uint16_t*)(kind == 0 ? p.q : kind == 1 ? p.k : p.v) +
+                                            token * (kind == 0 ? p.q_stride : kind == 1 ? p.k_stride : p.v_stride) + (long)min(h, heads - 1) * D, c);
+        };
+        u32x4 raw_next = load(part * per_part);   // (ahead of the position, which the angles wait for)
+        __builtin_amdgcn_sched_barrier(0);
         const int pos = p.positions[token];
         const bool there = pos >= 0 && pos < p.table_len;
         const long slot = APPEND ? (long)p.slots[b] + s : s;
@@ -109,19 +123,6 @@ __global__ __launch_bounds__(256) void slim_qk_norm_rope_kernel(const RopeArgs p
                 sn[i] = (double)ts[i];
             }
         }
-        // unit u's kind (uniform), and this lane's head of it: past the last one that head's again, which is not stored
-        auto unit = [&](int u, int& kind, int& heads, int& h) {
-            kind = u < uq ? 0 : u < uq + uk ? 1 : 2;
-            heads = kind == 0 ? p.q_heads : p.kv_heads;
-            h = (u - (kind == 0 ? 0 : kind == 1 ? uq : uq + uk)) * RW + sub;
-        };
-        auto load = [&](int u) {
-            int kind, heads, h;
-            unit(u, kind, heads, h);
-            return load_piece<D, PAIRS>((const uint16_t*)(kind == 0 ? p.q : kind == 1 ? p.k : p.v) +
-                                            token * (kind == 0 ? p.q_stride : kind == 1 ? p.k_stride : p.v_stride) + (long)min(h, heads - 1) * D, c);
-        };
-        u32x4 raw_next = load(part * per_part);
         if (!there) {   // (uniform) padding: rows of zeros, nothing into the cache, no more of its rows read
             for (int u = part * per_part; u < (APPEND ? min(u_end, uq) : u_end); ++u) {
                 int kind, heads, h;

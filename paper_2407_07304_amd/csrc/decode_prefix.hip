@@ -443,7 +443,9 @@ hipError_t launch_decode_prefix(const PrefixArgs& a, hipStream_t stream) {
         const integral_constant<int, 1> one{};
         const integral_constant<int, 4> four{};
         if (p.n_records <= 2 * RPW) return combine(one, integral_constant<int, 2>{});
-        if (p.n_records <= 4 * RPW) return combine(one, four);
+        // (a wave a row up to three passes, four beyond.  Four and one wave, us: 32 on 8 heads, 36 sequences, P=4096, 18 records 24.9 and 21.9; 48, P=2500,
+        // 12 23.5 and 20.2; 4 sequences, P=16000, 33 13.8 and 13.9; 2, P=16000, 33 12.5 and 13.0; 64 on 8, 5 sequences, 66 19.8 and 21.6)
+        if (p.n_records <= 12 * RPW) return combine(one, four);
         return combine(four, four);
     };
     return a.head_dim == 128 ? with_d(integral_constant<int, 128>{}) : with_d(integral_constant<int, 64>{});

@@ -313,7 +313,7 @@ __global__ __launch_bounds__(256, 2) void slim_decode_prefix_kernel(const Prefix
             f32x4 o[FORM][D / 16];
             float M[FORM], lsum[FORM];
             char* const kS = smem + w * GqaLds<D, FORM>::WAVE_BYTES;
-            gqa_sweep<D, 4, FORM>(kS, lane, [&](int i) { return p.q + row_of(min(i, n_rows - 1)) * D; }, p.pkc + kv0 * D, p.pks + kv0,
+            gqa_sweep<D, 4, FORM, false>(kS, lane, [&](int i) { return p.q + row_of(min(i, n_rows - 1)) * D; }, p.pkc + kv0 * D, p.pks + kv0,
                                          p.pvc + kv0 * D, p.pvs + kv0, p.P, first, first < end ? (end - first + 3) / 4 : 0, p.scale_log2e,
                                          nothing, o, M, lsum);
             gqa_record<D, FORM>(kS, lane, o, M, lsum);
@@ -340,7 +340,7 @@ __global__ __launch_bounds__(256, 2) void slim_decode_prefix_kernel(const Prefix
     f32x4 o[NC][D / 16];
     float M[NC], lsum[NC];
     char* const kS = smem + w * GqaLds<D, NC>::WAVE_BYTES;
-    gqa_sweep<D, 4, NC>(kS, lane, [&](int i) { return p.q + (row0 + min(i, heads - 1)) * D; }, p.kc + kv0 * D, p.ks + kv0, p.vc + kv0 * D,
+    gqa_sweep<D, 4, NC, false>(kS, lane, [&](int i) { return p.q + (row0 + min(i, heads - 1)) * D; }, p.kc + kv0 * D, p.ks + kv0, p.vc + kv0 * D,
                                p.vs + kv0, T, first, first < end ? (end - first + 3) / 4 : 0, p.scale_log2e, nothing, o, M, lsum);
     gqa_record<D, NC>(kS, lane, o, M, lsum);
     __syncthreads();

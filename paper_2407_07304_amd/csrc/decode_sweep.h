@@ -15,6 +15,12 @@ typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x2 __attribute__((ext_vector_type(2)));
 typedef __attribute__((address_space(3))) i32x2 lds_i32x2;
 
+// Two fp32 values as two bf16 each: the value rounded, and what that leaves (off by at most 2^-16 of the value together)
+__device__ __forceinline__ void pack_bf16x2_twice(float lo, float hi, unsigned& rounded, unsigned& rest) {
+    rounded = pack_bf16x2(lo, hi);
+    rest = pack_bf16x2(lo - bf16_bits_to_f32(rounded & 0xffffu), hi - __uint_as_float(rounded & 0xffff0000u));
+}
+
 // 8 INT8 codes -> 8 bf16, exact
 __device__ __forceinline__ bf16x8 widen8(const i32x2 cw) {
     u32x4 r;
@@ -40,8 +46,9 @@ struct GqaLds {
 // One wave's sweep: tiles first, first + W, ... (n_tiles of them) of the T tokens at kc, ks, vc, vs, for 16 NC columns.  q_row(i) is
 // column i's row of D query values.  Out: running max of this lane's column (log2 units), this lane's part of its sum, the
 // accumulators.  keep(nc, t0, u): sees the scores (log2 units; register 4 tt + r is token t0 + 16 tt + 4 lq + r) of every tile.
+// FINE: the second product takes a probability (times v_scale) as two bf16 and not as one: twice the matrix instructions.
 // kS: the wave's own LDS.
-template <int D, int W, int NC, class QRow, class Keep>
+template <int D, int W, int NC, bool FINE, class QRow, class Keep>
 __device__ __forceinline__ void gqa_sweep(char* const kS, const int lane, const QRow q_row, const int8_t* kc, const float* ks, const int8_t* vc,
                                           const float* vs, const int T, const int first, const int n_tiles, const float scale_log2e,
                                           const Keep keep, f32x4 (&o)[NC][D / 16], float (&M)[NC], float (&lsum)[NC]) {
@@ -151,7 +158,7 @@ __device__ __forceinline__ void gqa_sweep(char* const kS, const int lane, const 
                 kf[tt][s][0] = widen8(i32x2{kw[tt][s][0], kw[tt][s][1]});
                 kf[tt][s][1] = widen8(i32x2{kw[tt][s][2], kw[tt][s][3]});
             }
-        u32x4 pw[NC];
+        u32x4 pw[NC], rest[FINE ? NC : 1];
 #pragma unroll
         for (int nc = 0; nc < NC; ++nc) {
             f32x4 acc[2] = {{0.0f, 0.0f, 0.0f, 0.0f}, {0.0f, 0.0f, 0.0f, 0.0f}};
@@ -201,8 +208,18 @@ __device__ __forceinline__ void gqa_sweep(char* const kS, const int lane, const 
 #pragma unroll
             for (int tt = 0; tt < 2; ++tt) {
                 const f32x4 vf = *reinterpret_cast<const f32x4*>(&scS[32 + 16 * tt + 4 * lq]);
-                pw[nc][2 * tt] = pack_bf16x2(u[4 * tt] * vf[0], u[4 * tt + 1] * vf[1]);
-                pw[nc][2 * tt + 1] = pack_bf16x2(u[4 * tt + 2] * vf[2], u[4 * tt + 3] * vf[3]);
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const float a = u[4 * tt + 2 * i] * vf[2 * i], b = u[4 * tt + 2 * i + 1] * vf[2 * i + 1];
+                    if constexpr (FINE) {
+                        unsigned more, less;
+                        pack_bf16x2_twice(a, b, more, less);
+                        pw[nc][2 * tt + i] = more;
+                        rest[nc][2 * tt + i] = less;
+                    } else {
+                        pw[nc][2 * tt + i] = pack_bf16x2(a, b);
+                    }
+                }
             }
         }
 
@@ -212,8 +229,10 @@ __device__ __forceinline__ void gqa_sweep(char* const kS, const int lane, const 
             const i32x2 vw = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2*)(vS + v_addr + 16 * dt));
             const bf16x8 va = widen8(vw);
 #pragma unroll
-            for (int nc = 0; nc < NC; ++nc)
+            for (int nc = 0; nc < NC; ++nc) {
                 o[nc][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, __builtin_bit_cast(bf16x8, pw[nc]), o[nc][dt], 0, 0, 0);
+                if constexpr (FINE) o[nc][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, __builtin_bit_cast(bf16x8, rest[nc]), o[nc][dt], 0, 0, 0);
+            }
         }
     }
 }

@@ -117,6 +117,29 @@ def test_weights_long_caches(sa, B, Hq, Hkv, D, T):
 
 
 @gpu
+@pytest.mark.parametrize("B,Hq,Hkv,T", [(1, 8, 8, 33), (3, 4, 4, 700), (1, 32, 32, 3000), (100, 4, 4, 300), (2, 40, 1, 300), (1, 70, 1, 2500)])
+@pytest.mark.parametrize("D", [64, 128])
+def test_results_have_the_bits_of_the_decode_without_weights(sa, B, Hq, Hkv, T, D):
+    """One query head a KV head, or more than 32: the decode keeps its probabilities in fp32 there, and so does this one but for the last
+    of two roundings to bf16, 2^-16 of a probability.  What is left of the file's bound is 2^-16 + 2^-14 of sum_t p_t |v^_t| and the result's
+    own rounding."""
+    print("bits of the result", B, Hq, Hkv, T, D, flush=True)
+    rng = np.random.default_rng(B + Hq + T + D)
+    own = [*cache(rng, B, Hkv, T, D), *cache(rng, B, Hkv, T, D)]
+    lens = torch.from_numpy(rng.integers(1, T + 1, B).astype(np.int32))
+    lens[0] = T
+    q = torch.from_numpy(rng.standard_normal((B, Hq, 1, D), dtype=np.float32)).to(BF16)
+    scale = 1 / math.sqrt(D)
+    want, bound, _, _ = reference(q, own, lens, scale)
+    last = 2.0 ** -8 * (1 + 2.0 ** -8) * want.abs()
+    bound = last + (bound - last) * (2.0 ** -16 + 2.0 ** -14) / (2.0 ** -8 + 2.0 ** -14)
+    dev = (q.cuda(), *on_gpu(own), lens.cuda(), scale)
+    for out, what in ((sa.slim_attn_decode_int8_varlen(*dev), "without weights"), (sa.slim_attn_decode_int8_weights(*dev)[0], "with weights")):
+        off = (out.double().cpu() - want).abs()
+        assert (off <= bound).all(), "%s: %.3g of its bound" % (what, (off / bound).max())
+
+
+@gpu
 @pytest.mark.parametrize("B,Hq,Hkv,T", [(2, 8, 2, 700), (40, 12, 3, 333), (1, 20, 1, 2500)])
 def test_weights_of_sharp_rows_and_zero_tokens(sa, B, Hq, Hkv, T):
     """Rows that one token carries; a tenth of the tokens have a scale of zero, and so a score of zero and no value."""

@@ -309,8 +309,9 @@ int slim_qk_norm_rope_append_int8(const void* q_bf16, const void* k_bf16, const 
  * out_bf16  device, out  [batch, q_heads, 1, head_dim] bf16
  * workspace device, scratch, at least slim_attn_decode_int8_shared_prefix_workspace_bytes(...) bytes (0: the shape is invalid);
  *           contents before and after the call are meaningless; calls that may run at the same time need one each.
- * What lies past a sequence's length is never read into the result.  batch x kv_heads x splits, and batch x q_heads, must stay
- * below 2^24 (SLIM_ERR_SHAPE).  The result does not depend on the order in which workgroups finish.
+ * What lies past a sequence's length is never read into the result.  out and the workspace must not overlap each other or any other
+ * buffer (SLIM_ERR_OVERLAP).  batch x kv_heads x splits, and batch x q_heads, must stay below 2^24 (SLIM_ERR_SHAPE).  The result does not
+ * depend on the order in which workgroups finish.
  */
 size_t slim_attn_decode_int8_shared_prefix_workspace_bytes(int batch, int q_heads, int kv_heads, int prefix_len, int kv_len, int head_dim);
 int slim_attn_decode_int8_shared_prefix(const void* q_bf16, const int8_t* prefix_k_codes, const float* prefix_k_scale,
@@ -331,8 +332,8 @@ int slim_attn_decode_int8_shared_prefix(const void* q_bf16, const int8_t* prefix
  * weights_out  device, out  [batch, kv_heads, kv_len] fp32; may be weights_in: the sums over the steps of a sequence
  * workspace    device, scratch, at least slim_attn_decode_int8_weights_workspace_bytes(...) bytes (0: the shape is invalid): every
  *              score in fp32, and the splits' records; calls that may run at the same time need one each.
- * kv_lens is taken as in slim_attn_decode_int8_varlen (1 to kv_len); weights_out must not overlap any buffer but weights_in, and
- * that only if it is the same (SLIM_ERR_OVERLAP).  batch x kv_heads x splits must stay below 2^23 (SLIM_ERR_SHAPE).
+ * kv_lens is taken as in slim_attn_decode_int8_varlen (1 to kv_len); out, weights_out and the workspace must not overlap another buffer,
+ * but that weights_out may be weights_in (SLIM_ERR_OVERLAP).  batch x kv_heads x splits must stay below 2^23 (SLIM_ERR_SHAPE).
  */
 size_t slim_attn_decode_int8_weights_workspace_bytes(int batch, int q_heads, int kv_heads, int kv_len, int head_dim);
 int slim_attn_decode_int8_weights(const void* q_bf16, const int8_t* k_codes, const float* k_scale,

@@ -438,7 +438,13 @@ int slim_attn_decode_int8_shared_prefix(const void* q_bf16, const int8_t* prefix
     for (int i = 0; i < 11; ++i)
         if (misaligned(all[i])) return SLIM_ERR_ALIGN;
     if ((uintptr_t)kv_lens & 3u) return SLIM_ERR_ALIGN;
-    if (workspace_bytes < slim::decode_prefix_workspace_bytes(batch, q_heads, kv_heads, prefix_len, kv_len, head_dim)) return SLIM_ERR_WORKSPACE;
+    const size_t need = slim::decode_prefix_workspace_bytes(batch, q_heads, kv_heads, prefix_len, kv_len, head_dim);
+    if (workspace_bytes < need) return SLIM_ERR_WORKSPACE;
+    const size_t pre = (size_t)kv_heads * prefix_len, own = (size_t)batch * kv_heads * kv_len, q_bytes = (size_t)batch * q_heads * head_dim * 2;
+    const Range r[12] = {{out_bf16, q_bytes}, {workspace, need}, {q_bf16, q_bytes}, {prefix_k_codes, pre * head_dim}, {prefix_k_scale, pre * 4},
+                         {prefix_v_codes, pre * head_dim}, {prefix_v_scale, pre * 4}, {k_codes, own * head_dim}, {k_scale, own * 4},
+                         {v_codes, own * head_dim}, {v_scale, own * 4}, {kv_lens, (size_t)batch * 4}};
+    if (any_overlap(r, 2, 12)) return SLIM_ERR_OVERLAP;
     slim::PrefixArgs a;
     a.q = q_bf16;
     a.prefix_k_codes = prefix_k_codes, a.prefix_k_scale = prefix_k_scale, a.prefix_v_codes = prefix_v_codes, a.prefix_v_scale = prefix_v_scale;

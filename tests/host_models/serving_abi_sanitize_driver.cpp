@@ -73,6 +73,9 @@ int main() {
     expect(prefix(p_need, huge, 9000, huge, 0.1f, at(10)), SLIM_ERR_SHAPE, "prefix overflowing sizes");
     expect(prefix(p_need, 20, 9000, 700, 0.1f, at(10, 8)), SLIM_ERR_ALIGN, "prefix align");
     expect(prefix(p_need, 20, 9000, 700, 0.1f, nullptr), SLIM_ERR_NULL, "prefix null");
+    expect(prefix(p_need, 20, 9000, 700, 0.1f, at(11, 16)), SLIM_ERR_OVERLAP, "prefix into its workspace");
+    expect(prefix(p_need, 20, 9000, 700, 0.1f, at(9, 64)), SLIM_ERR_OVERLAP, "prefix over the lengths");
+    expect(prefix(p_need, 20, 9000, 700, 0.1f, at(8, -32)), SLIM_ERR_OVERLAP, "prefix over the scales");
 
     const size_t w_need = slim_attn_decode_int8_weights_workspace_bytes(3, 64, 8, 5000, 128);
     if (w_need < (size_t)3 * 64 * 5000 * 4) { std::fprintf(stderr, "weights workspace size\n"); ++bad; }

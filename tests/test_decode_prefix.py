@@ -317,6 +317,27 @@ def test_shared_prefix_refusals(sa):
     assert call(wsb=size(2, 4, 2, 100, 50, 128) - 1) == 5
 
 
+def test_shared_prefix_refuses_results_over_other_buffers(sa):
+    """The merge writes `out` while other workgroups read the records in `ws`, and the sweep writes `ws` while others read the caches."""
+    lib = sa.load()
+    B, Hq, Hkv, P, T, D, far = 2, 4, 2, 100, 50, 128, 0x1000000
+    need = lib.slim_attn_decode_int8_shared_prefix_workspace_bytes(B, Hq, Hkv, P, T, D)
+    size = {"q": B * Hq * D * 2, "pkc": Hkv * P * D, "pks": Hkv * P * 4, "pvc": Hkv * P * D, "pvs": Hkv * P * 4, "kc": B * Hkv * T * D,
+            "ks": B * Hkv * T * 4, "vc": B * Hkv * T * D, "vs": B * Hkv * T * 4, "lens": B * 4, "out": B * Hq * D * 2, "ws": need}
+    home = {n: (i + 1) * far for i, n in enumerate(size)}
+
+    def call(**other):
+        at = dict(home, **other)
+        return lib.slim_attn_decode_int8_shared_prefix(*(P_(at[n]) for n in size), need, B, Hq, Hkv, P, T, D, 0, 0.1, None)
+
+    for result in ("out", "ws"):
+        for n in size:
+            if n != result:
+                last = (size[n] - 1) // 16 * 16       # (the last 16 bytes of one, the first of the other)
+                assert call(**{result: home[n]}) == 7 and call(**{result: home[n] + last}) == 7, (result, n)
+                assert call(**{result: home[n] - (size[result] - 1) // 16 * 16}) == 7, (result, n)
+
+
 def test_shared_prefix_binding_refusals(sa):
     B, Hq, Hkv, D, P, T = 2, 4, 2, 64, 7, 5
 

@@ -259,7 +259,7 @@ __device__ __forceinline__ void prefix_sweep(char* const smem, const QRow q_row,
             for (int r4 = 0; r4 < 4; ++r4)
                 *reinterpret_cast<f32x4*>(ws_acc + idx * D + 32 * dt + 8 * r4 + 4 * hh) =
                     f32x4{o[dt][4 * r4], o[dt][4 * r4 + 1], o[dt][4 * r4 + 2], o[dt][4 * r4 + 3]};
-        if (hh == 0) reinterpret_cast<f32x2*>(ws_ml)[idx] = f32x2{first ? kNone : M, L};   // (nothing: behind everything)
+        if (hh == 0) reinterpret_cast<f32x2*>(ws_ml)[idx] = f32x2{first ? kMasked : M, L};   // (nothing: behind everything)
     }
 }
 

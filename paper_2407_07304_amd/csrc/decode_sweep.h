@@ -6,10 +6,6 @@
 
 namespace slim {
 
-// Stands for the maximum of nothing: finite, so that two of them differ by zero, and below any score (a difference that passes the
-// range of fp32 is -infinity, whose exponential is the zero that is wanted)
-constexpr float kNone = -3.0e38f;
-
 constexpr int kGqaTile = 32;    // tokens per tile
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x2 __attribute__((ext_vector_type(2)));
@@ -126,7 +122,7 @@ __device__ __forceinline__ void gqa_sweep(char* const kS, const int lane, const 
 
 #pragma unroll
     for (int nc = 0; nc < NC; ++nc) {
-        M[nc] = kNone;
+        M[nc] = kMasked;
         lsum[nc] = 0.0f;
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) o[nc][dt] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
@@ -178,7 +174,7 @@ __device__ __forceinline__ void gqa_sweep(char* const kS, const int lane, const 
             }
             if (t0 + kGqaTile > T) {   // the sequence ends inside this tile (or before it)
 #pragma unroll
-                for (int r = 0; r < 8; ++r) u[r] = (t0 + 16 * (r / 4) + 4 * lq + r % 4 < T) ? u[r] : kNone;
+                for (int r = 0; r < 8; ++r) u[r] = (t0 + 16 * (r / 4) + 4 * lq + r % 4 < T) ? u[r] : kMasked;
             }
             keep(nc, t0, u);
             float umax = fmaxf(u[0], u[1]);
@@ -264,7 +260,7 @@ template <int D, int W, int NC>
 __device__ __forceinline__ void gqa_merged(const char* const smem, const int h, const int d, float& acc, float& top, float& L) {
     constexpr int OPITCH = GqaLds<D, NC>::OPITCH, WAVE_BYTES = GqaLds<D, NC>::WAVE_BYTES;
     float m[W];
-    top = kNone;
+    top = kMasked;
 #pragma unroll
     for (int ww = 0; ww < W; ++ww) {
         m[ww] = reinterpret_cast<const float*>(smem + ww * WAVE_BYTES)[h];
@@ -286,7 +282,7 @@ __device__ __forceinline__ void gqa_merged(const char* const smem, const int h, 
 // come in with few, wide loads that are all issued before anything is computed: D/4 lanes read a record with one 128-bit
 // load each, a wave RPW = 256/D records at a time.  Up to U RPW records a row one wave does it, and a workgroup has four
 // rows; more are shared by the four waves of a workgroup and merged through LDS.  Slots past the last split re-read the last
-// one and count as empty (max = kNone, sum = 0); runs longer than the slots take another pass with a running (max, sum,
+// one and count as empty (max = kMasked, sum = 0); runs longer than the slots take another pass with a running (max, sum,
 // accumulator).  With a thread for every output value and sixteen records a thread (32-bit loads, 512 threads a row beyond sixteen
 // splits) the wide form's decode took, before -> now: 64 on 8 heads, T=32768, 32 splits 18.6 -> 16.1 us, D=64 14.7 -> 12.6; 8
 // heads, T=16000, 32 splits 11.8 -> 9.5; 32 heads, T=4000, 8 splits 9.5 -> 9.2; 16 sequences, 64 on 8 heads, T=8192, 2 splits 45.2 ->
@@ -297,7 +293,7 @@ __device__ __forceinline__ void combine_row(const f32x2* const ml, const f32x4* 
     constexpr int LPR = D / 4, RPW = 64 / LPR;
     const int c = lane % LPR, sub = lane / LPR, part = WAVES == 1 ? 0 : w;
     acc += c;
-    float M = kNone, L = 0.0f;
+    float M = kMasked, L = 0.0f;
     f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
     for (int s0 = 0; s0 < n_used; s0 += WAVES * RPW * U) {
         float m[U], l[U];
@@ -307,7 +303,7 @@ __device__ __forceinline__ void combine_row(const f32x2* const ml, const f32x4* 
             const int s = s0 + (i * WAVES + part) * RPW + sub, sp = min(s, n_used - 1);
             const f32x2 t = ml[sp];
             const f32x4 av = acc[(long)sp * LPR];
-            m[i] = s < n_used ? t[0] : kNone;
+            m[i] = s < n_used ? t[0] : kMasked;
             l[i] = s < n_used ? t[1] : 0.0f;
             a[i] = s < n_used ? av : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
         }
@@ -346,7 +342,7 @@ __device__ __forceinline__ void combine_row(const f32x2* const ml, const f32x4* 
         }
         __syncthreads();
         if (w != 0) return;
-        M = kNone;
+        M = kMasked;
 #pragma unroll
         for (int i = 0; i < WAVES; ++i) M = fmaxf(M, mS[i]);
         L = 0.0f;

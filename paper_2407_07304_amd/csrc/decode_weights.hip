@@ -164,7 +164,7 @@ __global__ __launch_bounds__(256) void slim_decode_weights_finish_kernel(const W
             // a head's maximum and sum over its records: 16 lanes a head
             for (int h = tid >> 4; h < heads; h += 16) {
                 const f32x2* const r = ml + (row0 + h0 + h) * p.n_split;
-                float m = kNone, l = 0.0f;
+                float m = kMasked, l = 0.0f;
                 for (int i = tid & 15; i < n_used; i += 16) {
                     const f32x2 v = r[i];
                     const float m_new = fmaxf(m, v[0]);

@@ -17,7 +17,9 @@ typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kMasked = -1.0e30f;  // finite stand-in for -inf: exp2(kMasked - m) == 0 for any finite m
+// The score of a masked key and the maximum of nothing: finite, so that two of them differ by zero, and below any score (a difference that
+// passes the range of fp32 is -infinity, whose exponential is the zero that is wanted)
+constexpr float kMasked = -3.0e38f;
 
 __device__ __forceinline__ float bf16_bits_to_f32(unsigned int bits16) { return __uint_as_float(bits16 << 16); }
 

@@ -261,7 +261,8 @@ int slim_attn_decode_int8_varlen(const void* q_bf16, const int8_t* k_codes, cons
  *     (y_i, y_j) -> (y_i c - y_j s, y_j c + y_i s),   c = cos_sin[p][i'], s = cos_sin[p][head_dim/2 + i'],  p = positions[b,s]
  * where pair i' of head_dim/2 is (i, j) = (i', i' + head_dim/2), or (2 i', 2 i' + 1) with interleaved == 1.  Keys likewise with
  * k_weight; values are only moved.  Every result is the exact value, as 64-bit arithmetic gives it, rounded to fp32 and then
- * to bf16.  A token whose position lies outside [0, table_len) (the padding of a batch: -1) gets rows of zeros.
+ * to bf16, also where a row is not finite: an infinity makes the mean infinite, so that with a norm its pair is NaN and the row's
+ * other values are zero.  A token whose position lies outside [0, table_len) (the padding of a batch: -1) gets rows of zeros.
  * q, k, v   device, in   rows of q_heads (k, v: kv_heads) x head_dim bf16, densely packed for each token; token b * seq_len + s
  *           begins q_stride (k_stride, v_stride) values after the one before: a multiple of 8, at least the row's own length
  *           and below 2^31.  (One projection's output [batch, seq_len, q_heads + 2 kv_heads, head_dim] is three such tensors.)

@@ -42,12 +42,14 @@ __device__ __forceinline__ double row_group_sum(double v) {
     return v;
 }
 
-// 1 / sqrt(a), a > 0 and normal: the hardware's estimate (some 24 bits) and two steps of Newton's method
+// 1 / sqrt(a), a > 0: the hardware's estimate (some 24 bits) and two steps of Newton's method.  The estimate of an infinity is 0, which
+// no step takes further (infinity times 0 is not a number).
 __device__ __forceinline__ double inverse_root(double a) {
-    double y = __builtin_amdgcn_rsq(a);
+    const double estimate = __builtin_amdgcn_rsq(a);
+    double y = estimate;
 #pragma unroll
     for (int i = 0; i < 2; ++i) y = fma(y, fma(-a * y, 0.5 * y, 0.5), y);
-    return y;
+    return estimate == 0.0 ? estimate : y;
 }
 
 // The first of a result's two roundings, to fp32 and from there to bf16.  (Contracted, the compiler makes one of the two, which is

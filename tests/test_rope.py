@@ -167,6 +167,48 @@ def test_rows_of_extreme_values(sa, D, interleaved):
 
 
 @gpu
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("norm", [True, False])
+def test_rows_that_are_not_finite(sa, oracle, D, interleaved, norm):
+    """A row with an infinity has the mean square infinity: its values become zeros, the pair that holds the infinity NaN; without a norm,
+    and with a NaN, the formula's values too.  The other rows, and their codes, are as ever."""
+    rng = np.random.default_rng(D)
+    B, S, H, length, T = 2, 9, 5, 40, 12
+    qkv, (qw, kw), positions = case(rng, B, S, H, H, D, length, norm)
+    positions[0, 0] = 0                                       # (cosines of one, sines of zero)
+    positions[1, 8] = -1                                      # padding, an infinity in it or not
+    x = bf16_bits_to_f32(qkv)
+    bad = np.zeros((B, S, 2 * H), bool)
+    for b, s, h, d, v in ((0, 0, 1, 3, np.inf), (0, 1, 6, D - 1, -np.inf), (0, 2, 2, 0, np.nan), (1, 3, 9, D // 2, np.inf), (1, 8, 0, 1, np.inf),
+                          (1, 4, 4, 7, np.inf), (1, 4, 4, 8, -np.inf), (1, 5, 7, 2, np.nan)):
+        x[b, s, h, d] = v
+        bad[b, s, h] = True
+    qkv = f32_to_bf16_bits(x)
+    qkv[np.isnan(x)] = 0x7fc0
+    table, slots = table_of(length, D), np.array([0, 3], np.int32)
+    args = [torch.from_numpy(table).cuda(), torch.from_numpy(positions).cuda()]
+    out = sa.slim_qk_norm_rope(*views(dev(qkv), H, H), *args, *on_device((qw, kw)), 1e-6, interleaved)
+    cache = [torch.zeros((B, H, T, D), dtype=I8, device="cuda"), torch.zeros((B, H, T), device="cuda"),
+             torch.zeros((B, H, T, D), dtype=I8, device="cuda"), torch.zeros((B, H, T), device="cuda")]
+    q2 = sa.slim_qk_norm_rope_append_int8(*views(dev(qkv), H, H), *args, torch.from_numpy(slots).cuda(), *cache, *on_device((qw, kw)), 1e-6,
+                                          interleaved)
+    with np.errstate(invalid="ignore"):
+        want = [rotated(h, w, table, positions, 1e-6, interleaved) for h, w in zip(views(qkv, H, H)[:2], (qw, kw))]
+    for got, w, what in ((out[0], want[0], "q"), (out[1], want[1], "k"), (q2, want[0], "q, with the append")):
+        g, w = bf16_bits_to_f32(host(got)), bf16_bits_to_f32(w)
+        assert np.array_equal(np.isnan(g), np.isnan(w)), what
+        assert np.array_equal(g[~np.isnan(w)], w[~np.isnan(w)]), what
+    codes, scales = oracle.kv_quant_int8(np.ascontiguousarray(np.where(bad[:, :, H:].transpose(0, 2, 1)[..., None], 0, want[1]).astype(np.uint16)))
+    for b in range(B):
+        for s in range(S):
+            if positions[b, s] >= 0:
+                fine = ~bad[b, s, H:]
+                assert np.array_equal(cache[0][b, :, slots[b] + s].cpu().numpy()[fine], codes[b, :, s][fine])
+                assert np.array_equal(cache[1][b, :, slots[b] + s].cpu().numpy()[fine], scales[b, :, s][fine])
+
+
+@gpu
 def test_one_of_the_norms_and_tensors_of_their_own(sa):
     """Keys normed and queries not, and the other way round; q, k and v as tensors of their own, and as every other row of one."""
     rng = np.random.default_rng(6)

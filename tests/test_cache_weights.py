@@ -140,6 +140,24 @@ def test_results_have_the_bits_of_the_decode_without_weights(sa, B, Hq, Hkv, T, 
 
 
 @gpu
+@pytest.mark.parametrize("B,Hq,Hkv,D,T", [(40, 280, 4, 64, 1100), (37, 320, 8, 128, 1030)])
+@pytest.mark.parametrize("weights", [False, True])
+def test_weights_of_rows_dealt_by_length(sa, B, Hq, Hkv, D, T, weights):
+    """More than 32 query heads a KV head in as many rows (sequences x head groups) as are dealt by their lengths, which are spread: each
+    row is a (KV head, head group), with a record of its own, and the second launch turns all groups' scores into weights."""
+    print("rows dealt by length", B, Hq, Hkv, D, T, weights, flush=True)
+    groups = Hkv * ((Hq // Hkv + 31) // 32)
+    ranked, through = ctypes.c_int(), ctypes.c_int()
+    assert sa.load().slim_attn_decode_int8_plan_options(B, 32 * groups, groups, T, D, 1, ctypes.byref(ranked), ctypes.byref(through)) == 0
+    assert ranked.value == 1
+    rng = np.random.default_rng(T)
+    own = [*cache(rng, B, Hkv, T, D), *cache(rng, B, Hkv, T, D)]
+    lens = torch.from_numpy(np.where(rng.random(B) < 0.25, T, rng.integers(T // 8, T + 1, B)).astype(np.int32))
+    q = torch.from_numpy(rng.standard_normal((B, Hq, 1, D), dtype=np.float32)).to(BF16)
+    check(sa, q, own, lens, 1 / math.sqrt(D), "dealt", torch.from_numpy(rng.random((B, Hkv, T), dtype=np.float32)) if weights else None)
+
+
+@gpu
 @pytest.mark.parametrize("B,Hq,Hkv,T", [(2, 8, 2, 700), (40, 12, 3, 333), (1, 20, 1, 2500)])
 def test_weights_of_sharp_rows_and_zero_tokens(sa, B, Hq, Hkv, T):
     """Rows that one token carries; a tenth of the tokens have a scale of zero, and so a score of zero and no value."""

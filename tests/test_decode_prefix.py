@@ -118,6 +118,37 @@ def test_shared_prefix_many_splits(sa, B, Hq, Hkv, D, P, T):
 
 
 @gpu
+@pytest.mark.parametrize("B,Hq,Hkv,D,P,T,records", [(130, 128, 128, 64, 4200, 3, 3), (70, 256, 256, 128, 4097, 2, 3), (40, 256, 256, 128, 4300, 1, 5),
+                                                    (20, 512, 256, 64, 5000, 2, 5)])
+def test_shared_prefix_in_twice_as_many_splits(sa, B, Hq, Hkv, D, P, T, records):
+    """A workgroup a compute unit has 64 stages or more: two are launched, each with a split of its own (records a row: theirs, of up to
+    64 rows two a split, and the own cache's)."""
+    print("shared prefix", B, Hq, Hkv, D, P, T, flush=True)
+    assert sa.slim_attn_decode_int8_shared_prefix_workspace_bytes(B, Hq, Hkv, P, T, D) == B * Hq * records * (D + 2) * 4
+    gen = torch.Generator(device="cuda").manual_seed(P)
+
+    def random_cache(*shape):
+        return (torch.randint(-127, 128, shape, generator=gen, device="cuda", dtype=I8),
+                0.02 * torch.rand(shape[:-1], generator=gen, device="cuda") + 0.005)
+
+    prefix, own = [*random_cache(1, Hkv, P, D), *random_cache(1, Hkv, P, D)], [*random_cache(B, Hkv, T, D), *random_cache(B, Hkv, T, D)]
+    q = torch.randn((B, Hq, 1, D), generator=gen, device="cuda").to(BF16)
+    lens = torch.randint(0, T + 1, (B,), generator=gen, device="cuda", dtype=I32)
+    scale = 1 / math.sqrt(D)
+    got = sa.slim_attn_decode_int8_shared_prefix(q, *prefix, *own, lens, scale).double().view(B, Hkv, -1, D)
+    past = (torch.arange(T, device="cuda") >= lens[:, None])[:, None]
+    for g in range(Hkv):
+        rows = q.double().view(B, Hkv, -1, D)[:, g]
+        (pk, pv), (k, v) = (((x[0][i, g].double() * x[1][i, g].double()[..., None]), (x[2][i, g].double() * x[3][i, g].double()[..., None]))
+                            for x, i in ((prefix, 0), (own, slice(None))))
+        s = torch.cat([rows @ pk.T, (rows[:, :, None] * k[:, None]).sum(-1).masked_fill(past, -math.inf)], 2) * scale
+        p = torch.softmax(s, 2)
+        want, bound = (p[:, :, :P] @ f(pv) + (p[:, :, P:, None] * f(v)[:, None]).sum(2) for f in (lambda x: x, torch.abs))
+        bound = (2.0 ** -8 + 2.0 ** -14) * bound + 2.0 ** -8 * (1 + 2.0 ** -8) * want.abs()
+        assert ((got[:, g] - want).abs() <= bound).all(), g
+
+
+@gpu
 @pytest.mark.parametrize("B,Hq,Hkv", [(2, 8, 2), (8, 8, 2), (12, 8, 2), (40, 8, 2), (90, 8, 2)])
 @pytest.mark.parametrize("D", [64, 128])
 def test_shared_prefix_sharp_rows(sa, B, Hq, Hkv, D):

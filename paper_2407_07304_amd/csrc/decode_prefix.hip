@@ -107,6 +107,7 @@ __device__ __forceinline__ void prefix_sweep(char* const smem, const QRow q_row,
         for (int r = 0; r < 16; ++r) o[dt][r] = 0.0f;
     float M = 0.0f, lsum = 0.0f;   // running max of this lane's row (log2 units), this lane's part of the row sum
     bool first = true;             // (uniform)
+    float move_above = -INFINITY;  // what a score relative to the running max passes where that moves (uniform; 8 behind the first stage)
 
     const std::integral_constant<int, 0> set0{};
     const std::integral_constant<int, 1> set1{};
@@ -185,33 +186,64 @@ __device__ __forceinline__ void prefix_sweep(char* const smem, const QRow q_row,
         fetch_v(0);
         issue(std::integral_constant<int, turn ^ 1>{}, t0 + 3 * STAGE);   // (here, where registers are free again)
         __builtin_amdgcn_sched_barrier(0);
-        if (t0 + STAGE > T) {
+        auto masked_max = [&]() __attribute__((always_inline)) {   // (masks what lies past the end)
+            if (t0 + STAGE > T) {
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) u[t][r] = t0 + tile0 + 32 * t + 8 * (r / 4) + 4 * hh + r % 4 < T ? u[t][r] : -INFINITY;
+            }
+            float top = u[0][0];
 #pragma unroll
             for (int t = 0; t < NT; ++t)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) u[t][r] = t0 + tile0 + 32 * t + 8 * (r / 4) + 4 * hh + r % 4 < T ? u[t][r] : -INFINITY;
-        }
-        float umax = u[0][0];
-#pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-            for (int r = 0; r < 16; r += 2) umax = fmaxf(umax, fmaxf(u[t][r], u[t][r + 1]));
+                for (int r = 0; r < 16; r += 2) top = fmaxf(top, fmaxf(u[t][r], u[t][r + 1]));
+            return top;
+        };
+        const float umax = masked_max();
         // the running max, a whole number (decode_gqa.hip says why), moves only when a score has passed it by 2^8, but for the first
-        // stage, which sets it (not if the wave's tile of it is past the end: it has no other)
-        if (t0 + tile0 < T && (first || __builtin_amdgcn_ballot_w64(umax > 8.0f) != 0)) {
-            const float up = ceilf(half_max(umax)), by = first ? up : fmaxf(up, 0.0f);
-            const float alpha = first ? 0.0f : fast_exp2(-by);   // (nothing to rescale yet)
+        // stage, which sets it (not if the wave's tile of it is past the end, all -infinity: it has no other)
+        if (__builtin_expect(__builtin_amdgcn_ballot_w64(umax > move_above) != 0, 0)) {
+            const float up = ceilf(half_max(umax));
+            float by = first ? up : fmaxf(up, 0.0f), m_new = M + by;
+            float alpha = first ? 0.0f : fast_exp2(-by);   // (nothing to rescale yet)
+            if (__builtin_expect(!first && __builtin_amdgcn_ballot_w64(umax > 256.0f) != 0, 0)) {
+                // Scores so far above it have lost their last bits to the running max (all of them where that is below -2^24): once more,
+                // without it
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) u[t][r] = 0.0f;
+#pragma unroll
+                    for (int s = 0; s < KS; ++s) {
+                        u[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(kS + k_addr + t * 32 * PITCHK + 32 * s), qB[s],
+                                                                       u[t], 0, 0, 0);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+#pragma unroll
+                    for (int r4 = 0; r4 < 4; ++r4) {
+                        const f32x4 f = *reinterpret_cast<const f32x4*>(scS + 32 * t + 8 * r4);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) u[t][4 * r4 + e] *= f[e];
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                }
+                by = m_new = fmaxf(ceilf(half_max(masked_max())), M);
+                alpha = fast_exp2(M - m_new);
+            }
 #pragma unroll
             for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) o[dt][r] *= alpha;
             lsum *= alpha;
-            M += by;
+            M = m_new;
 #pragma unroll
             for (int t = 0; t < NT; ++t)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) u[t][r] -= by;
             first = false;
+            move_above = 8.0f;
         }
         // O^T += V^T P^T: k-step x covers tokens 16 x + {4 hh .. 4 hh + 3} and 16 x + 8 + {4 hh .. 4 hh + 3}, registers 8 x to 8 x + 7; the
         // probabilities take their token's v_scale before they are rounded to bf16, operands of the product

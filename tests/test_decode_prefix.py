@@ -218,6 +218,24 @@ def test_shared_prefix_of_extreme_queries(sa, B, Hq, Hkv, D):
 
 
 @gpu
+@pytest.mark.parametrize("B,Hq,Hkv", [(2, 8, 2), (6, 8, 2), (12, 8, 2), (40, 8, 2)])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("low", [2.0 ** 8, 2.0 ** 14, 2.0 ** 60])
+def test_shared_prefix_behind_tokens_of_far_lower_scores(sa, B, Hq, Hkv, D, low):
+    """Every other 64 tokens of the prefix have scores `low` times the others' size, all negative: a running maximum that such tokens set
+    leaves little of the others' scores in fp32, or nothing, if it is taken off them before they have moved it."""
+    rng = np.random.default_rng(B + D)
+    P, T, scale = 1500, 40, 1 / math.sqrt(D)
+    prefix, own = [*cache(rng, 1, Hkv, P, D), *cache(rng, 1, Hkv, P, D)], [*cache(rng, B, Hkv, T, D), *cache(rng, B, Hkv, T, D)]
+    far = torch.arange(P) // 64 % 2 == 0
+    prefix[0][:, :, far] = -prefix[0][:, :, far].abs().clamp(min=32)
+    prefix[1][:, :, far] *= low
+    q = queries(rng, B, Hq, D).abs()
+    lens = torch.from_numpy(rng.integers(0, T + 1, B).astype(np.int32))
+    check(sa, q, prefix, own, lens, scale, "%g below" % low)
+
+
+@gpu
 @pytest.mark.parametrize("B", [2, 6, 12, 40])
 def test_shared_prefix_of_very_low_scores(sa, B):
     """All scores of a row around -2^100, where they are all the same in fp32: the mean of the values, without what lies past the end."""

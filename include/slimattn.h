@@ -11,8 +11,11 @@
  *
  * and, around them, what a serving loop needs: kv_quant_int8_pair (K and V in one launch),
  * kv_quant_int8_append (one new token per sequence into the cache), slim_attn_prefill_emit_int8 (prefill that also writes the
- * cache), slim_attn_decode_int8_varlen (a batch whose caches differ in length), plus
- * slim_attn_prefill_two_sweep and slim_attn_prefill_strip, two comparison variants of the prefill that keep the
+ * cache), slim_attn_decode_int8_varlen (a batch whose caches differ in length),
+ * slim_attn_decode_int8_static (a decode without a workspace), slim_qk_norm_rope and slim_qk_norm_rope_append_int8 (norm and
+ * rotation of queries and keys, K and V into the cache or not), slim_attn_decode_int8_shared_prefix (sequences behind one prompt that
+ * is cached once), slim_attn_decode_int8_weights and slim_cache_evict_int8 (attention weights of cached tokens, and the eviction by
+ * them), plus slim_attn_prefill_two_sweep and slim_attn_prefill_strip, two comparison variants of the prefill that keep the
  * paper's own order of operations (the whole score row before the softmax).
  *
  * Common rules

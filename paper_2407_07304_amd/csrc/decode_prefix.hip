@@ -5,7 +5,7 @@
 //
 // a softmax over both parts, which only the merge of the records joins.  The prefix's part is, for each KV head, a product of
 // (batch x query heads of the KV head) rows: the cache is read once for 128 of them in the place of once a sequence, and from
-// some 200 rows on the matrix cores bound it.  The own part is what it is in any decode: bound by memory.  Both are one
+// some 200 rows on vector issue bounds it, beside the matrix cores.  The own part is what it is in any decode: bound by memory.  Both are one
 // launch, the prefix's workgroups first, so that the one's arithmetic runs beside the other's loads.
 //
 // A workgroup (four waves) of the prefix has a run of its tokens for
@@ -15,6 +15,9 @@
 //     transpose read.  Up to 64 rows, two waves have the rows and two the same rows over every other tile, with records
 //     of their own.
 // One of the own caches has a run of a (sequence, KV head)'s tokens for its query heads, up to 32.
+// Probabilities times v_scale are operands of the second product, rounded to bf16, as in the prefill and the grouped decode: each is off by
+// up to 2^-8 of itself, a result by some 1.4 times what its own rounding to bf16 makes.  As two bf16 each they would cost the shared tiles
+// a fifth (64 sequences, 64 on 8 heads, P=32768 98 -> 118 us; 48, 32 on 8, P=8192, T=1000 34.0 -> 37.2).
 #include <algorithm>
 #include <type_traits>
 
@@ -410,7 +413,8 @@ static PrefixPlan prefix_plan(int batch, int q_heads, int kv_heads, int prefix_l
     // (64 on 8 heads, 64 sequences, P=32768 107 and 93 us); and none with less than 4 stages, 8 from 2048 query rows on, as every one
     // costs a record of its rows besides (with 4, 8 and 16 stages 32 on 8 heads, 48 sequences, P=1024, T=100 14.3, 18.6 and 27.9 us; 128
     // sequences, P=2000 27.8, 21.2 and 29.3; 32 heads, 128 sequences, P=2000 43.7, 38.3 and 36.6).  Up to 32 rows a record is little: two
-    // tiles a wave (32 on 8 heads, 2 sequences, P=4000, T=100 14.0 us with 8, 11.0 with 4, 9.5).
+    // tiles a wave (32 on 8 heads, 2 sequences, P=4000, T=100 14.0 us with 8, 11.0 with 4, 9.5).  (All of 128 codes a token; calls of 64
+    // follow the same rule.)
     const int phases = plan.form == 3 ? 2 : 1;
     const long items = (long)kv_heads * plan.row_blocks, stages = ((long)prefix_len + (plan.form < 3 ? 127 : 63)) / (plan.form < 3 ? 128 : 64);
     long n = (256 + items - 1) / items;
@@ -476,7 +480,8 @@ hipError_t launch_decode_prefix(const PrefixArgs& a, hipStream_t stream) {
         const integral_constant<int, 4> four{};
         if (p.n_records <= 2 * RPW) return combine(one, integral_constant<int, 2>{});
         // (a wave a row up to three passes, four beyond.  Four and one wave, us: 32 on 8 heads, 36 sequences, P=4096, 18 records 24.9 and 21.9; 48, P=2500,
-        // 12 23.5 and 20.2; 4 sequences, P=16000, 33 13.8 and 13.9; 2, P=16000, 33 12.5 and 13.0; 64 on 8, 5 sequences, 66 19.8 and 21.6)
+        // 12 23.5 and 20.2; 4 sequences, P=16000, 33 13.8 and 13.9; 2, P=16000, 33 12.5 and 13.0; 64 on 8, 5 sequences, 66 19.8 and 21.6:
+        // all of 128 codes, where a pass of four loads is 8 records)
         if (p.n_records <= 12 * RPW) return combine(one, four);
         return combine(four, four);
     };

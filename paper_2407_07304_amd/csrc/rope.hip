@@ -195,7 +195,7 @@ hipError_t launch_qk_norm_rope(const RopeArgs& a, bool append, hipStream_t strea
     const long tokens = (long)a.batch * a.seq_len;
     // a wave for each unit of heads where tokens are few, up to six units a wave (its position, angles and weights once) where
     // that leaves 8192 waves: 32 heads, 2048 tokens 29.9 us with one unit a wave, 25.2 with two, 23.6 with six, 28.7 with twelve; 8192
-    // tokens, 64 on 8 heads 94.4, 75.0, 72.1, 72.3
+    // tokens, 64 on 8 heads 94.4, 75.0, 72.1, 72.3 (three sets of inputs and of results in turn, so that neither stays in the caches)
     long per = tokens * units / 8192;
     per = per < 1 ? 1 : per > 6 ? 6 : per;
     const int parts = (units + (int)per - 1) / (int)per;

@@ -330,8 +330,7 @@ int slim_attn_decode_int8_shared_prefix(const void* q_bf16, const int8_t* prefix
  * head: what slim_cache_evict_int8 goes by.
  *     weights_out[b,g,t] = weights_in[b,g,t] + sum_{h reads g} softmax_t(s[b,h,:])     for t < kv_lens[b], and 0 past it
  * The weights are fp32, of the unrounded probabilities.  (A token that is appended later thus starts at 0.)  For out the probabilities
- * times v_scale enter the second product as they do in that call with 2 to 32 query heads a KV head, rounded to bf16, and otherwise,
- * where it keeps them in fp32, as two bf16 each (off by at most 2^-16 of their value).
+ * times v_scale enter the second product as two bf16 each (off by at most 2^-16 of their value), whatever the number of query heads.
  * weights_in   device, in   [batch, kv_heads, kv_len] fp32, or NULL (zeros)
  * weights_out  device, out  [batch, kv_heads, kv_len] fp32; may be weights_in: the sums over the steps of a sequence
  * workspace    device, scratch, at least slim_attn_decode_int8_weights_workspace_bytes(...) bytes (0: the shape is invalid): every

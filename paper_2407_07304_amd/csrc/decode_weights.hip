@@ -12,10 +12,10 @@
 // each, a second launch does, beside the merge of their records.  A lone query head a KV head takes this kernel too: 15 of the 16 columns of
 // its products are empty, but the cache's bytes are the same.
 //
-// Results are as exact as those of the decode without weights.  That rounds the probabilities (times v_scale) to bf16 where 2 to 32 query heads
-// share a KV head and keeps them in fp32 where one or more than 32 do; so here the second product takes them as one bf16 in the former case
-// and as two, 16 bits of them, in the latter (FINE), whose distance from the 64-bit result is otherwise 1.4 times the other's.  It costs 2 to
-// 3 %: one bf16 and two, 32 heads, T=1000 7.7 and 7.9 us, 8 sequences, T=4000 33.2 and 34.2; 16 sequences, 40 on 1 heads, T=9000 29.8 and 30.8.
+// Results have the bits of fp32 probabilities: the second product takes a probability (times its v_scale) as two bf16, 16 bits of it.  (Rounded
+// to one, as in the decode of 2 to 32 query heads a KV head without weights, a result is 1.4 times as far from the 64-bit one; the decode of
+// one head, or more than 32, has them in fp32.)  It costs 0 to 4 %: one bf16 and two, 32 heads, T=1000 7.7 and 7.9 us, 8 sequences, T=4000
+// 33.2 and 34.2, on another card 37.2 and 38.9; 16 sequences, 64 on 8 heads, T=8192 45.9 and 46.5, 64 codes 31.1 and 30.9, 40 on 1 heads, T=9000 29.8 and 30.8.
 #include <algorithm>
 #include <type_traits>
 
@@ -67,8 +67,8 @@ __device__ __forceinline__ void store_weights(const float* w_in, float* w_out, i
     }
 }
 
-// D head dimension, W waves, NC groups of 16 heads; WHOLE: a workgroup has all of a (sequence, KV head)'s tokens and heads; FINE: gqa_sweep
-template <int D, int W, int NC, bool WHOLE, bool FINE>
+// D head dimension, W waves, NC groups of 16 heads; WHOLE: a workgroup has all of a (sequence, KV head)'s tokens and heads
+template <int D, int W, int NC, bool WHOLE>
 __global__ __launch_bounds__(64 * W) void slim_decode_weights_kernel(const WeightsParams p) {
     constexpr int WAVE_BYTES = GqaLds<D, NC>::WAVE_BYTES;
     __shared__ __attribute__((aligned(16))) char smem[W * WAVE_BYTES];
@@ -99,7 +99,7 @@ __global__ __launch_bounds__(64 * W) void slim_decode_weights_kernel(const Weigh
 
     f32x4 o[NC][D / 16];
     float M[NC], lsum[NC];
-    gqa_sweep<D, W, NC, FINE>(kS, lane, [&](int i) { return p.q + (row0 + min(i, heads - 1)) * D; }, p.kc + kvrow0 * D, p.ks + kvrow0,
+    gqa_sweep<D, W, NC, true>(kS, lane, [&](int i) { return p.q + (row0 + min(i, heads - 1)) * D; }, p.kc + kvrow0 * D, p.ks + kvrow0,
                                p.vc + kvrow0 * D, p.vs + kvrow0, T, first, first < end ? (end - first + W - 1) / W : 0, p.scale_log2e,
                                [&](int nc, int t0, const float (&u)[8]) {
                                    // (through a descriptor over the tile's rows: the columns past the last head store nothing, and the store is the
@@ -230,24 +230,16 @@ hipError_t launch_decode_weights(const DecodeArgs& a, const float* w_in, float* 
     using std::integral_constant;
     auto with_d = [&](auto d_c) {
         constexpr int D = decltype(d_c)::value, RPW = 256 / D;
-        auto launch = [&](auto w_c, auto nc_c, auto whole_c, auto fine_c) {
-            constexpr int W = decltype(w_c)::value;
-            hipLaunchKernelGGL((slim_decode_weights_kernel<D, W, decltype(nc_c)::value, decltype(whole_c)::value, decltype(fine_c)::value>), grid,
-                               dim3(64 * W), 0, stream, p);
+        auto sweep = [&](auto w_c, auto nc_c) {
+            constexpr int W = decltype(w_c)::value, NC = decltype(nc_c)::value;
+            if (whole) hipLaunchKernelGGL((slim_decode_weights_kernel<D, W, NC, true>), grid, dim3(64 * W), 0, stream, p);
+            else hipLaunchKernelGGL((slim_decode_weights_kernel<D, W, NC, false>), grid, dim3(64 * W), 0, stream, p);
             return hipGetLastError();
         };
         const integral_constant<int, 1> one{};
-        const integral_constant<int, 2> two{};
         const integral_constant<int, 4> four{};
         const integral_constant<int, 8> eight{};
-        auto sweep = [&](auto w_c, auto nc_c, auto fine_c) {
-            return whole ? launch(w_c, nc_c, std::true_type{}, fine_c) : launch(w_c, nc_c, std::false_type{}, fine_c);
-        };
-        auto few = [&](auto fine_c) { return plan.waves == 8 ? sweep(eight, one, fine_c) : sweep(four, one, fine_c); };
-        const hipError_t e = p.G > 32   ? launch(eight, two, std::false_type{}, std::true_type{})   // (several head groups are never whole)
-                             : p.G > 16 ? sweep(eight, two, std::false_type{})
-                             : p.G > 1  ? few(std::false_type{})
-                                        : few(std::true_type{});
+        const hipError_t e = p.G > 16 ? sweep(eight, integral_constant<int, 2>{}) : plan.waves == 8 ? sweep(eight, one) : sweep(four, one);
         if (e != hipSuccess || whole) return e;
         const int chunks = (a.kv_len + kWeightsChunk - 1) / kWeightsChunk;
         auto finish = [&](auto waves_c, auto u_c) {

@@ -158,6 +158,25 @@ def test_weights_of_rows_dealt_by_length(sa, B, Hq, Hkv, D, T, weights):
 
 
 @gpu
+@pytest.mark.parametrize("B,Hq,Hkv,T", [(1, 8, 4, 33), (3, 32, 8, 700), (60, 16, 2, 300), (1, 64, 8, 5000), (2, 20, 1, 2500), (100, 32, 1, 200)])
+@pytest.mark.parametrize("D", [64, 128])
+def test_results_of_grouped_heads_have_the_bits_of_fp32(sa, B, Hq, Hkv, T, D):
+    """2 to 32 query heads a KV head: the same bound, which the decode without weights, whose probabilities are one bf16 each there, does not
+    hold."""
+    print("bits of the result", B, Hq, Hkv, T, D, flush=True)
+    rng = np.random.default_rng(B + Hq + T + D)
+    own = [*cache(rng, B, Hkv, T, D), *cache(rng, B, Hkv, T, D)]
+    lens = torch.from_numpy(rng.integers(1, T + 1, B).astype(np.int32))
+    lens[0] = T
+    q = torch.from_numpy(rng.standard_normal((B, Hq, 1, D), dtype=np.float32)).to(BF16)
+    want, bound, _, _ = reference(q, own, lens, 1 / math.sqrt(D))
+    last = 2.0 ** -8 * (1 + 2.0 ** -8) * want.abs()
+    bound = last + (bound - last) * (2.0 ** -16 + 2.0 ** -14) / (2.0 ** -8 + 2.0 ** -14)
+    off = (sa.slim_attn_decode_int8_weights(q.cuda(), *on_gpu(own), lens.cuda(), 1 / math.sqrt(D))[0].double().cpu() - want).abs()
+    assert (off <= bound).all(), "%.3g of its bound" % (off / bound).max()
+
+
+@gpu
 @pytest.mark.parametrize("B,Hq,Hkv,T", [(2, 8, 2, 700), (40, 12, 3, 333), (1, 20, 1, 2500)])
 def test_weights_of_sharp_rows_and_zero_tokens(sa, B, Hq, Hkv, T):
     """Rows that one token carries; a tenth of the tokens have a scale of zero, and so a score of zero and no value."""

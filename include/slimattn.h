@@ -304,7 +304,8 @@ int slim_qk_norm_rope_append_int8(const void* q_bf16, const void* k_bf16, const 
  *     s_t over the prefix's prefix_len tokens and then the sequence's first kv_lens[b] own tokens, as in slim_attn_decode_int8
  *     o[b,h,:] = sum_t softmax_t(s) * v^_t
  * one softmax over both parts.  The prefix is read once for up to 128 query rows (batch x query heads of a KV head) and its
- * products run on the matrix cores; probabilities times v_scale are rounded to bf16 before the second product.
+ * products run on the matrix cores.  With up to 16 such rows probabilities times v_scale enter the second product as two bf16 each (off
+ * by at most 2^-16 of their value), with more they are rounded to bf16 before it, as in slim_attn_prefill.
  * q_bf16    device, in   [batch, q_heads, 1, head_dim] bf16
  * prefix_k_codes, prefix_v_codes  device, in  [kv_heads, prefix_len, head_dim] int8 (what slim_attn_prefill_emit_int8 writes for a
  *           batch of one);  prefix_k_scale, prefix_v_scale  [kv_heads, prefix_len] fp32

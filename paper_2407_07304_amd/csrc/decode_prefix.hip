@@ -15,9 +15,12 @@
 //     transpose read.  Up to 64 rows, two waves have the rows and two the same rows over every other tile, with records
 //     of their own.
 // One of the own caches has a run of a (sequence, KV head)'s tokens for its query heads, up to 32.
-// Probabilities times v_scale are operands of the second product, rounded to bf16, as in the prefill and the grouped decode: each is off by
-// up to 2^-8 of itself, a result by some 1.4 times what its own rounding to bf16 makes.  As two bf16 each they would cost the shared tiles
-// a fifth (64 sequences, 64 on 8 heads, P=32768 98 -> 118 us; 48, 32 on 8, P=8192, T=1000 34.0 -> 37.2).
+// Probabilities times v_scale are operands of the second product.  Up to 16 rows, where memory and latency bound the call, they are two bf16
+// each and results have the bits of fp32 probabilities; 14 shapes took 4 % less to 2 % more than with one (4 sequences, 32 on 8 heads, P=1000
+// 9.4 and 9.5 us, P=30000 19.0 both; 16, 32 heads, P=4000, T=2000 38.2 and 39.0).  Above, they are rounded to one, as in the prefill and the
+// grouped decode: each is off by up to 2^-8 of itself, a result by 1.4 times what its own rounding to bf16 makes.  Two would cost up to 9 % with
+// 32 rows (8 sequences, 32 on 8 heads, P=30000 22.5 -> 24.2) and a fifth with more (64, 64 on 8, P=32768 98 -> 118; 48, 32 on 8, P=8192, T=1000
+// 34.0 -> 37.2).
 #include <algorithm>
 #include <type_traits>
 
@@ -348,7 +351,7 @@ __global__ __launch_bounds__(256, 2) void slim_decode_prefix_kernel(const Prefix
             f32x4 o[FORM][D / 16];
             float M[FORM], lsum[FORM];
             char* const kS = smem + w * GqaLds<D, FORM>::WAVE_BYTES;
-            gqa_sweep<D, 4, FORM, false>(kS, lane, [&](int i) { return p.q + row_of(min(i, n_rows - 1)) * D; }, p.pkc + kv0 * D, p.pks + kv0,
+            gqa_sweep<D, 4, FORM, FORM == 1>(kS, lane, [&](int i) { return p.q + row_of(min(i, n_rows - 1)) * D; }, p.pkc + kv0 * D, p.pks + kv0,
                                          p.pvc + kv0 * D, p.pvs + kv0, p.P, first, first < end ? (end - first + 3) / 4 : 0, p.scale_log2e,
                                          nothing, o, M, lsum);
             gqa_record<D, FORM>(kS, lane, o, M, lsum);
@@ -375,7 +378,7 @@ __global__ __launch_bounds__(256, 2) void slim_decode_prefix_kernel(const Prefix
     f32x4 o[NC][D / 16];
     float M[NC], lsum[NC];
     char* const kS = smem + w * GqaLds<D, NC>::WAVE_BYTES;
-    gqa_sweep<D, 4, NC, false>(kS, lane, [&](int i) { return p.q + (row0 + min(i, heads - 1)) * D; }, p.kc + kv0 * D, p.ks + kv0, p.vc + kv0 * D,
+    gqa_sweep<D, 4, NC, FORM == 1>(kS, lane, [&](int i) { return p.q + (row0 + min(i, heads - 1)) * D; }, p.kc + kv0 * D, p.ks + kv0, p.vc + kv0 * D,
                                p.vs + kv0, T, first, first < end ? (end - first + 3) / 4 : 0, p.scale_log2e, nothing, o, M, lsum);
     gqa_record<D, NC>(kS, lane, o, M, lsum);
     __syncthreads();
@@ -466,7 +469,7 @@ hipError_t launch_decode_prefix(const PrefixArgs& a, hipStream_t stream) {
         auto with_form = [&](auto form_c) {
             return p.G > 16 ? sweep(form_c, integral_constant<int, 2>{}) : sweep(form_c, integral_constant<int, 1>{});
         };
-        const hipError_t e = plan.form == 1   ? with_form(integral_constant<int, 1>{})
+        const hipError_t e = plan.form == 1   ? sweep(integral_constant<int, 1>{}, integral_constant<int, 1>{})   // (16 rows: no more heads)
                              : plan.form == 2 ? with_form(integral_constant<int, 2>{})
                              : plan.form == 3 ? with_form(integral_constant<int, 3>{})
                                               : with_form(integral_constant<int, 4>{});

@@ -107,6 +107,26 @@ def test_shared_prefix_small_shapes(sa, B, Hq, Hkv, D, P, T):
 
 
 @gpu
+@pytest.mark.parametrize("B,Hq,Hkv,P,T", [(1, 4, 4, 700, 64), (4, 32, 8, 1000, 64), (2, 40, 8, 33, 900), (3, 16, 4, 9000, 5), (16, 2, 2, 300, 500), (1, 16, 1, 500, 70)])
+@pytest.mark.parametrize("D", [64, 128])
+def test_shared_prefix_of_few_rows_has_the_bits_of_fp32(sa, B, Hq, Hkv, P, T, D):
+    """Up to 16 rows a KV head: a probability times its v_scale enters the second product as two bf16, off by 2^-16.  What is left of the
+    file's bound is 2^-16 + 2^-14 of sum_t p_t |v^_t| and the result's own rounding."""
+    print("shared prefix", B, Hq, Hkv, D, P, T, flush=True)
+    rng = np.random.default_rng(B + Hq + P + T + D)
+    prefix, own = [*cache(rng, 1, Hkv, P, D), *cache(rng, 1, Hkv, P, D)], [*cache(rng, B, Hkv, T, D), *cache(rng, B, Hkv, T, D)]
+    lens = torch.from_numpy(rng.integers(0, T + 1, B).astype(np.int32))
+    lens[0] = T
+    q = queries(rng, B, Hq, D)
+    want, bound = reference(q, prefix, own, lens, 1 / math.sqrt(D))
+    last = 2.0 ** -8 * (1 + 2.0 ** -8) * want.abs()
+    bound = last + (bound - last) * (2.0 ** -16 + 2.0 ** -14) / (2.0 ** -8 + 2.0 ** -14)
+    got = sa.slim_attn_decode_int8_shared_prefix(q.cuda(), *on_gpu(prefix), *on_gpu(own), lens.cuda(), 1 / math.sqrt(D))
+    off = (got.double().cpu() - want).abs()
+    assert (off <= bound).all(), "%.3g of its bound" % (off / bound).max()
+
+
+@gpu
 @pytest.mark.parametrize("B,Hq,Hkv,D,P,T", [(4, 32, 8, 128, 9000, 64), (48, 32, 8, 128, 5000, 1000), (24, 64, 8, 64, 7001, 513),
                                             (1, 32, 32, 128, 20000, 1), (12, 16, 2, 64, 12345, 2000)])
 def test_shared_prefix_many_splits(sa, B, Hq, Hkv, D, P, T):

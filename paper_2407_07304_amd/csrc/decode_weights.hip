@@ -5,8 +5,9 @@
 //
 // The softmax's maximum and sum are known at the end of the sweep only, so the sweep of the grouped decode (decode_sweep.h)
 // leaves its scores, fp32, in the workspace: 4 bytes a query head and token beside the 2 (D + 4) of the cache, written once and read
-// once.  The writes are what the sweep takes longer for than a plain decode's: 16 sequences, 64 on 8 heads, T=8192 all full 41.9 and 54 us
-// of kernel, 43.4 with the same stores into one small piece of memory; past the L2 or through it they cost as much or more.  (K again
+// once.  The writes are what the sweep takes longer for than a plain decode's: 16 sequences, 64 on 8 heads, T=8192 all full 42 and 56 us
+// of kernel (with one bf16 a probability 54, and 43.4 with the same stores into one small piece of memory); past the L2 or through it they cost as
+// much or more.  (K again
 // in the place of the scores would be D bytes and the first product again.)  Where one workgroup has a
 // whole (sequence, KV head), it turns its own scores into weights as soon as its waves are merged; where several have a part
 // each, a second launch does, beside the merge of their records.  A lone query head a KV head takes this kernel too: 15 of the 16 columns of

@@ -210,7 +210,7 @@ __device__ __forceinline__ void prefix_sweep(char* const smem, const QRow q_row,
         // the running max, a whole number (decode_gqa.hip says why), moves only when a score has passed it by 2^8, but for the first
         // stage, which sets it (not if the wave's tile of it is past the end, all -infinity: it has no other)
         if (__builtin_expect(__builtin_amdgcn_ballot_w64(umax > move_above) != 0, 0)) {
-            const float up = ceilf(half_max(umax));
+            const float up = fmaxf(ceilf(half_max(umax)), kMasked);   // (-infinity, of scores below what fp32 holds, cannot be taken off one)
             float by = first ? up : fmaxf(up, 0.0f), m_new = M + by;
             float alpha = first ? 0.0f : fast_exp2(-by);   // (nothing to rescale yet)
             if (__builtin_expect(!first && __builtin_amdgcn_ballot_w64(umax > 256.0f) != 0, 0)) {

@@ -240,10 +240,11 @@ def test_shared_prefix_of_extreme_queries(sa, B, Hq, Hkv, D):
 @gpu
 @pytest.mark.parametrize("B,Hq,Hkv", [(2, 8, 2), (6, 8, 2), (12, 8, 2), (40, 8, 2)])
 @pytest.mark.parametrize("D", [64, 128])
-@pytest.mark.parametrize("low", [2.0 ** 8, 2.0 ** 14, 2.0 ** 60])
+@pytest.mark.parametrize("low", [2.0 ** 8, 2.0 ** 14, 2.0 ** 60, 2.0 ** 127])
 def test_shared_prefix_behind_tokens_of_far_lower_scores(sa, B, Hq, Hkv, D, low):
     """Every other 64 tokens of the prefix have scores `low` times the others' size, all negative: a running maximum that such tokens set
-    leaves little of the others' scores in fp32, or nothing, if it is taken off them before they have moved it."""
+    leaves little of the others' scores in fp32, or nothing, if it is taken off them before they have moved it.  (Of 2^127 the scores are
+    below what fp32 holds: -infinity, a weight of zero all the same.)"""
     rng = np.random.default_rng(B + D)
     P, T, scale = 1500, 40, 1 / math.sqrt(D)
     prefix, own = [*cache(rng, 1, Hkv, P, D), *cache(rng, 1, Hkv, P, D)], [*cache(rng, B, Hkv, T, D), *cache(rng, B, Hkv, T, D)]
@@ -253,6 +254,8 @@ def test_shared_prefix_behind_tokens_of_far_lower_scores(sa, B, Hq, Hkv, D, low)
     q = queries(rng, B, Hq, D).abs()
     lens = torch.from_numpy(rng.integers(0, T + 1, B).astype(np.int32))
     check(sa, q, prefix, own, lens, scale, "%g below" % low)
+    q[:, ::3] = 0.0     # (and beside them rows that have these tokens' scores at zero, like all others')
+    check(sa, q, prefix, own, lens, scale, "%g below, but for some rows" % low)
 
 
 @gpu
